@@ -1,0 +1,302 @@
+// Eviction by accumulated attention weight (e2s_cache_evict), in two launches.
+//
+// evict_select_kernel, one workgroup per (sequence, key head): the tokens between the
+// first `sinks` and the last `recent` are ranked by a 32-bit key that orders floats as
+// integers (larger weight, larger key; NaN lowest), and the want-th largest key is found
+// digit by digit (11, 11 and 10 bits) from a histogram in LDS.  Tokens above it stay, and
+// of those equal to it the first ones; counts per wave and a scan over the waves place the
+// kept tokens in ascending order.  All decisions are on integers, so nothing depends on
+// the order of the atomic increments.  Each pass reads the weights again: 4 bytes per
+// token, from L2 after the first.
+//
+// evict_move_kernel, one workgroup per (sequence, key head, new block, keys or values):
+// gathers the block's kept rows, takes their largest magnitude to the block's scale, and
+// writes them rescaled by the ratio of two powers of two.  It moves each kept byte once.
+#include "serve_device.h"
+#include "serve_kernels.h"
+
+namespace e2s {
+namespace {
+
+constexpr int kSelThreads = 1024;
+constexpr int kSelWaves = kSelThreads / kWave;
+constexpr int kBins = 2048;
+
+struct EvictArgs {
+    const int32_t* pages;
+    const int32_t* lengths;
+    const float* weights;
+    const int32_t* new_pages;
+    int32_t* keep;
+    int32_t* new_len;
+    float* left;                     // or null
+    const uint8_t* src[2];
+    uint8_t* dst[2];
+    float* scale[2];
+    int64_t page_stride[2];
+    int64_t pages_stride, new_pages_stride;
+    int64_t ws[2], ls[2];
+    int G, P, K, W, sinks, recent, max_tokens, max_pages, num_pages, blocks;
+};
+
+__device__ __forceinline__ int evict_length(const EvictArgs& a, int64_t b) {
+    const int64_t cap = min(static_cast<int64_t>(a.max_pages) * a.P,
+                            static_cast<int64_t>(a.max_tokens));
+    return static_cast<int>(min(static_cast<int64_t>(max(a.lengths[b], 0)), cap));
+}
+
+// Larger weight, larger key; -0 as 0; NaN below everything.
+__device__ __forceinline__ uint32_t rank_key(float w) {
+    return w != w ? 0u : ordered_bits(w + 0.0f);
+}
+
+__global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
+    __shared__ uint32_t hist[kBins];
+    __shared__ uint32_t sums[kSelWaves];
+    __shared__ uint32_t ties[kSelWaves];
+    __shared__ uint32_t found[2];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int64_t b = blockIdx.x / a.G;
+    const int g = static_cast<int>(blockIdx.x - b * a.G);
+    const int n = evict_length(a, b);
+    const int kept = min(n, a.K);
+    const float* w = a.weights + b * a.ws[0] + g * a.ws[1];
+    int32_t* keep = a.keep + (b * a.G + g) * static_cast<int64_t>(a.K);
+    float* left = a.left ? a.left + b * a.ls[0] + g * a.ls[1] : nullptr;
+    if (g == 0 && tid == 0) a.new_len[b] = kept;
+    for (int j = kept + tid; j < a.K; j += kSelThreads) keep[j] = -1;
+    if (left)
+        for (int j = kept + tid; j < a.W; j += kSelThreads) left[j] = 0.0f;
+    if (n <= a.K) {
+        for (int j = tid; j < n; j += kSelThreads) {
+            keep[j] = j;
+            if (left) left[j] = w[j];
+        }
+        return;
+    }
+    // sinks + recent <= K < n: the ends do not meet, and m0 < m1
+    const int m0 = a.sinks, m1 = n - a.recent;
+    uint32_t want = static_cast<uint32_t>(a.K - a.sinks - a.recent);
+    // keys above `limit` stay, and of the keys equal to it the first `want`
+    uint32_t limit = 0xFFFFFFFFu;
+    if (want > 0) {
+        limit = 0;
+        uint32_t known = 0;                            // mask of the digits found
+#pragma unroll 1
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const uint32_t mask = pass == 2 ? 1023u : 2047u;
+            for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+            __syncthreads();
+            for (int i = m0 + tid; i < m1; i += kSelThreads) {
+                const uint32_t key = rank_key(w[i]);
+                if ((key & known) == limit) atomicAdd(&hist[(key >> shift) & mask], 1u);
+            }
+            __syncthreads();
+            // thread t owns bins 2047 - 2t and 2046 - 2t: sums from the top
+            const uint32_t h1 = hist[kBins - 1 - 2 * tid], h0 = hist[kBins - 2 - 2 * tid];
+            uint32_t run = h1 + h0;
+            for (int o = 1; o < kWave; o <<= 1) {
+                const uint32_t v = __shfl_up(run, o);
+                if (lane >= o) run += v;
+            }
+            if (lane == kWave - 1) sums[wave] = run;
+            __syncthreads();
+            uint32_t above = run - (h1 + h0);
+            for (int v = 0; v < wave; ++v) above += sums[v];
+            // the digit at which the count from the top reaches `want`
+            if (above < want && above + h1 + h0 >= want) {
+                const bool upper = above + h1 >= want;
+                found[0] = static_cast<uint32_t>(kBins - 1 - 2 * tid - (upper ? 0 : 1));
+                found[1] = want - above - (upper ? 0 : h1);
+            }
+            __syncthreads();
+            limit |= found[0] << shift;
+            want = found[1];
+            known |= mask << shift;
+            __syncthreads();
+        }
+    }
+    // every wave takes a run of tokens, whole groups of 64
+    const int per = (n + kSelThreads - 1) / kSelThreads * kWave;
+    const int i0 = wave * per, i1 = min(n, i0 + per);
+    uint32_t more = 0, same = 0;
+    for (int i = i0 + lane; i - lane < i1; i += kWave) {
+        bool up = false, tie = false;
+        if (i < i1) {
+            up = i < m0 || i >= m1;
+            if (!up) {
+                const uint32_t key = rank_key(w[i]);
+                up = key > limit;
+                tie = key == limit;
+            }
+        }
+        more += __popcll(__ballot(up));
+        same += __popcll(__ballot(tie));
+    }
+    if (lane == 0) {
+        sums[wave] = more;
+        ties[wave] = same;
+    }
+    __syncthreads();
+    more = same = 0;
+    for (int v = 0; v < wave; ++v) {
+        more += sums[v];
+        same += ties[v];
+    }
+    for (int i = i0 + lane; i - lane < i1; i += kWave) {
+        bool up = false, tie = false;
+        float x = 0.0f;
+        if (i < i1) {
+            x = w[i];
+            up = i < m0 || i >= m1;
+            if (!up) {
+                const uint32_t key = rank_key(x);
+                up = key > limit;
+                tie = key == limit;
+            }
+        }
+        const uint64_t ups = __ballot(up), equal = __ballot(tie);
+        const uint64_t below = (uint64_t{1} << lane) - 1;
+        const uint32_t before = same + __popcll(equal & below);
+        if (up || (tie && before < want)) {       // K tokens in all, so slot < K
+            const uint32_t slot = more + __popcll(ups & below) + min(before, want);
+            keep[slot] = i;
+            if (left) left[slot] = x;
+        }
+        more += __popcll(ups);
+        same += __popcll(equal);
+    }
+}
+
+// PACKETS packets of 16 bytes per thread cover a block.
+template <int D, int THREADS, int PACKETS>
+__global__ __launch_bounds__(THREADS) void evict_move_kernel(const EvictArgs a) {
+    constexpr int kLanes = D / 16;
+    __shared__ float shared[THREADS / kWave];
+    const int which = blockIdx.x & 1;
+    const int64_t unit = blockIdx.x >> 1;
+    const int g = static_cast<int>(unit % a.G);
+    const int64_t ub = unit / a.G;
+    const int64_t b = ub / a.blocks;
+    const int blk = static_cast<int>(ub - b * a.blocks);
+    const int kept = min(evict_length(a, b), a.K);
+    const int first = blk * a.P;
+    if (first >= kept) return;
+    const int page = a.new_pages[b * a.new_pages_stride + blk];
+    if (page < 0 || page >= a.num_pages) return;
+    const int rows = min(kept - first, a.P);
+    const int32_t* keep = a.keep + (b * a.G + g) * static_cast<int64_t>(a.K) + first;
+    const int64_t head = static_cast<int64_t>(g) * a.P * D;
+
+    u32x4 x[PACKETS];
+    float from[PACKETS];
+    float top = 0.0f;
+#pragma unroll
+    for (int p = 0; p < PACKETS; ++p) {
+        const int i = p * THREADS + threadIdx.x;
+        const int r = i / kLanes, c = i - r * kLanes;
+        x[p] = u32x4{0u, 0u, 0u, 0u};
+        from[p] = 1.0f;
+        if (r >= rows) continue;
+        const int idx = keep[r];                    // 0 <= idx < length <= max_pages * P
+        const int src = a.pages[b * a.pages_stride + idx / a.P];
+        if (src < 0 || src >= a.num_pages) continue;
+        from[p] = a.scale[which][static_cast<int64_t>(src) * a.G + g];
+        x[p] = *reinterpret_cast<const u32x4*>(a.src[which] + src * a.page_stride[which] + head +
+                                               static_cast<int64_t>(idx % a.P) * D + c * 16);
+    }
+#pragma unroll
+    for (int p = 0; p < PACKETS; ++p) {
+        const uint32_t word[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float v[4];
+            from_e4m3(word[i], v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)             // a NaN is no maximum
+                top = fmaxf(top, v[k] == v[k] ? fabsf(v[k]) * from[p] : 0.0f);
+        }
+    }
+    top = block_max<THREADS>(top, shared);
+    const float to = block_scale(top);
+    uint8_t* out = a.dst[which] + page * a.page_stride[which] + head;
+#pragma unroll
+    for (int p = 0; p < PACKETS; ++p) {
+        const int i = p * THREADS + threadIdx.x;
+        if (i / kLanes >= rows) continue;
+        u32x4 w = x[p];
+        if (from[p] != to) {
+            const float ratio = scale_ratio(from[p], to);
+            w.x = rescale_e4m3(w.x, ratio);
+            w.y = rescale_e4m3(w.y, ratio);
+            w.z = rescale_e4m3(w.z, ratio);
+            w.w = rescale_e4m3(w.w, ratio);
+        }
+        *(reinterpret_cast<u32x4*>(out) + i) = w;
+    }
+    if (threadIdx.x == 0) a.scale[which][static_cast<int64_t>(page) * a.G + g] = to;
+}
+
+template <int D, int THREADS, int PACKETS>
+void launch_move_k(const EvictArgs& a, int64_t B, hipStream_t st) {
+    hipLaunchKernelGGL((evict_move_kernel<D, THREADS, PACKETS>),
+                       dim3(static_cast<unsigned>(2 * B * a.blocks * a.G)), dim3(THREADS), 0, st,
+                       a);
+}
+
+template <int D>
+void launch_move(const EvictArgs& a, int64_t B, hipStream_t st) {
+    const int packets = a.P * (D / 16);             // 64 .. 1024
+    if (packets <= 64) launch_move_k<D, 64, 1>(a, B, st);
+    else if (packets <= 256) launch_move_k<D, 256, 1>(a, B, st);
+    else if (packets <= 512) launch_move_k<D, 256, 2>(a, B, st);
+    else launch_move_k<D, 256, 4>(a, B, st);
+}
+
+}  // namespace
+
+hipError_t launch_cache_evict(const e2s_cache& c, const e2s_cache_evict_shape& s,
+                              const int32_t* pages, const int32_t* lengths, const float* weights,
+                              const int32_t* new_pages, int32_t* keep_idx, int32_t* new_len,
+                              float* left, hipStream_t st) {
+    EvictArgs a{};
+    a.pages = pages;
+    a.lengths = lengths;
+    a.weights = weights;
+    a.new_pages = new_pages;
+    a.keep = keep_idx;
+    a.new_len = new_len;
+    a.left = left;
+    a.src[0] = a.dst[0] = static_cast<uint8_t*>(c.k);
+    a.src[1] = a.dst[1] = static_cast<uint8_t*>(c.v);
+    a.scale[0] = c.k_scale;
+    a.scale[1] = c.v_scale;
+    a.page_stride[0] = c.k_page_stride;
+    a.page_stride[1] = c.v_page_stride;
+    a.pages_stride = s.pages_stride;
+    a.new_pages_stride = s.new_pages_stride;
+    for (int i = 0; i < 2; ++i) {
+        a.ws[i] = s.weights_stride[i];
+        a.ls[i] = s.left_stride[i];
+    }
+    a.G = c.num_kv_heads;
+    a.P = c.page_tokens;
+    a.K = s.budget;
+    a.W = s.left_tokens;
+    a.sinks = s.sinks;
+    a.recent = s.recent;
+    a.max_tokens = s.max_tokens;
+    a.max_pages = s.max_pages;
+    a.num_pages = c.num_pages;
+    a.blocks = (s.budget + c.page_tokens - 1) / c.page_tokens;
+    hipLaunchKernelGGL(evict_select_kernel, dim3(static_cast<unsigned>(s.batch * a.G)),
+                       dim3(kSelThreads), 0, st, a);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    if (c.head_dim == 64) launch_move<64>(a, s.batch, st);
+    else launch_move<128>(a, s.batch, st);
+    return hipGetLastError();
+}
+
+}  // namespace e2s
