@@ -215,20 +215,41 @@ def _device_of(*tensors):
     raise ValueError(f"all tensors of a call must be on one GPU (got {sorted(map(str, devs))})")
 
 
+# The current device and its current stream as raw values.  The public functions return
+# objects, whose making costs more than the rest of a call; both forms read the same state.
+_CURRENT_DEVICE = getattr(_TORCH._C, "_cuda_getDevice", None) if _TORCH else None
+_CURRENT_STREAM = getattr(_TORCH._C, "_cuda_getCurrentRawStream", None) if _TORCH else None
+if _TORCH and (_CURRENT_DEVICE is None or _CURRENT_STREAM is None):
+    def _CURRENT_DEVICE():
+        return _TORCH.cuda.current_device()
+
+    def _CURRENT_STREAM(index):
+        return _TORCH.cuda.current_stream(index).cuda_stream
+
+
 def _launch(where: str, tensors, fn, *args, stream=None):
     """fn(*args, stream) with the tensors' device current (kernels are launched on
     that device), on its current stream unless one is given; raises on a status."""
-    torch = _torch()
-    dev = _device_of(*tensors)
+    index = -1
+    for t in tensors:
+        if t is not None:
+            i = t.get_device()
+            if index < 0:
+                index = i
+            if i != index or i < 0:
+                index = -1
+                break
+    if index < 0:
+        # no GPU tensor, or not one device: say which
+        raise ValueError(f"all tensors of a call must be on one GPU (got {_device_of(*tensors)})")
     # entering a device that is current already costs as much as a launch
-    if dev.type == "cuda" and torch.cuda.current_device() == dev.index:
-        st = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
-        status = fn(*args, st)
+    if _CURRENT_DEVICE() == index:
+        status = fn(*args, _CURRENT_STREAM(index) if stream is None else stream)
     else:
-        with torch.cuda.device(dev):
-            st = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
-            status = fn(*args, st)
-    _raise(status, where)
+        with _TORCH.cuda.device(index):
+            status = fn(*args, _CURRENT_STREAM(index) if stream is None else stream)
+    if status != OK:
+        _raise(status, where)
 
 
 def _raise(status: int, where: str):

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 from . import _lib
@@ -79,13 +80,12 @@ def _ref(t):
 
 SIGNATURES = {
     "e2s_rotary_plan_init": [_ref(RotarySpec), _ref(RotaryPlan)],
-    "e2s_rotate_positions": [_ref(RotaryShape), _ref(RotaryPlan), _P, _P, _P, _P, _P, _P],
-    "e2s_cache_append": [_ref(CacheDesc), _ref(AppendShape), _P, _P, _P, _P, _P, _P, _P],
-    "e2s_cache_attend_workspace_size": [_ref(CacheDesc), _ref(AttendShape),
-                                        _ref(ctypes.c_size_t)],
-    "e2s_cache_attend": [_ref(CacheDesc), _ref(AttendShape), _P, _P, _P, _P, _P, _P, _P, _P,
+    "e2s_rotate_positions": [_P, _ref(RotaryPlan), _P, _P, _P, _P, _P, _P],
+    "e2s_cache_append": [_ref(CacheDesc), _P, _P, _P, _P, _P, _P, _P, _P],
+    "e2s_cache_attend_workspace_size": [_ref(CacheDesc), _P, _ref(ctypes.c_size_t)],
+    "e2s_cache_attend": [_ref(CacheDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P,
                          ctypes.c_size_t, _P],
-    "e2s_cache_evict": [_ref(CacheDesc), _ref(EvictShape), _P, _P, _P, _P, _P, _P, _P, _P],
+    "e2s_cache_evict": [_ref(CacheDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P],
     "e2s_serve_abi_version": [],
 }
 for _name, _args in SIGNATURES.items():
@@ -94,26 +94,46 @@ for _name, _args in SIGNATURES.items():
 _LIB = _lib.lib()
 
 
+# What a step passes is packed in the records' layout (native sizes and alignment): one call
+# in place of one per field.
+_ROTARY = struct.Struct("@6i15q")
+_APPEND = struct.Struct("@6i7q")
+_ATTEND = struct.Struct("@8ifi11q")
+_EVICT = struct.Struct("@8i6q")
+
+
 def _rows(t, name, dtype=None):
-    """A [B, H, T, d] tensor of rows: any strides, the last dimension contiguous."""
-    _check(t, name, dtype=dtype, ndim=4, contiguous=False)
-    if t.stride(3) != 1 and t.shape[3] > 1:
+    """The strides of a [B, H, T, d] tensor of rows: any, the last dimension contiguous."""
+    if not (isinstance(t, _torch().Tensor) and t.is_cuda and t.dim() == 4 and
+            (dtype is None or t.dtype is dtype)):
+        _check(t, name, dtype=dtype, ndim=4, contiguous=False)
+    st = t.stride()
+    if st[3] != 1 and t.shape[3] > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
+    return st
 
 
 def _vector(t, name, n):
-    """An int32 [n] of per-sequence numbers."""
+    """The address of an int32 [n] of per-sequence numbers."""
     torch = _torch()
-    _check(t, name, dtype=torch.int32, ndim=1)
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.int32 and
+            t.dim() == 1 and t.is_contiguous()):
+        _check(t, name, dtype=torch.int32, ndim=1)
     if t.shape[0] != n:
         raise ValueError(f"{name} must be [{n}] (got {tuple(t.shape)})")
+    return t.data_ptr()
 
 
 def _table(t, name, n):
+    """The width and the row stride of an int32 [n, max_pages]."""
     torch = _torch()
-    _check(t, name, dtype=torch.int32, ndim=2, contiguous=False)
-    if t.shape[0] != n or t.shape[1] < 1 or (t.stride(1) != 1 and t.shape[1] > 1):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.int32 and
+            t.dim() == 2):
+        _check(t, name, dtype=torch.int32, ndim=2, contiguous=False)
+    (rows, width), st = t.shape, t.stride()
+    if rows != n or width < 1 or (st[1] != 1 and width > 1):
         raise ValueError(f"{name} must be [{n}, max_pages] with contiguous rows")
+    return width, st[0]
 
 
 # ---------------------------------------------------------------------------
@@ -148,45 +168,54 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
-    outs = []
+    dtype, B, T, D = x.dtype, x.shape[0], x.shape[2], plan.head_dim
+    heads, strides, out_strides, ptrs, outs = [], [], [], [], []
     for t, name, o in ((q, "q", q_out), (k, "k", k_out)):
         if t is None:
             if o is not None:
                 raise ValueError(f"{name}_out without {name}")
+            heads.append(0)
+            strides += (0, 0, 0)
+            out_strides += (0, 0, 0)
+            ptrs += (None, None)
             outs.append(None)
             continue
-        _rows(t, name, x.dtype)
-        if t.shape[0] != x.shape[0] or t.shape[2] != x.shape[2] or t.shape[3] != plan.head_dim:
-            raise ValueError(f"{name} {tuple(t.shape)} must be [B, heads, T, {plan.head_dim}] "
+        st = _rows(t, name, dtype)
+        shape = t.shape
+        if shape[0] != B or shape[2] != T or shape[3] != D:
+            raise ValueError(f"{name} {tuple(shape)} must be [B, heads, T, {D}] "
                              "with one B and T")
         if o is None:
             o = torch.empty_like(t)
+            so = o.stride()
         else:
-            _rows(o, name + "_out", x.dtype)
-            if o.shape != t.shape:
+            so = _rows(o, name + "_out", dtype)
+            if o.shape != shape:
                 raise ValueError(f"{name}_out must have {name}'s shape")
-            if o.data_ptr() == t.data_ptr() and o.stride() != t.stride():
+            if o.data_ptr() == t.data_ptr() and so != st:
                 raise ValueError(f"{name}_out in the place of {name} must have its strides")
+        heads.append(shape[1])
+        strides += st[:3]
+        out_strides += so[:3]
+        ptrs += (t.data_ptr(), o.data_ptr())
         outs.append(o)
-    B, T = x.shape[0], x.shape[2]
-    _check(positions, "positions", dtype=torch.int32, contiguous=False)
+    if not (isinstance(positions, torch.Tensor) and positions.is_cuda and
+            positions.dtype is torch.int32):
+        _check(positions, "positions", dtype=torch.int32, contiguous=False)
     lead = (3,) if plan.axes == 3 else ()
-    if tuple(positions.shape) not in (lead + (T,), lead + (B, T)):
+    shape, ps = positions.shape, positions.stride()
+    if shape == lead + (B, T):
+        ps = (ps[0] if lead else 0, ps[-2], ps[-1])
+    elif shape == lead + (T,):
+        ps = (ps[0] if lead else 0, 0, ps[-1])
+    else:
         raise ValueError(f"positions must be {list(lead + (T,))} or {list(lead + (B, T))} "
-                         f"(got {list(positions.shape)})")
-    ps = positions.stride()
-    sh = RotaryShape(B, T, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1],
-                     _dtype_code(x), int(bool(inverse)))
-    for t, o, si, so in ((q, outs[0], sh.q_stride, sh.q_out_stride),
-                         (k, outs[1], sh.k_stride, sh.k_out_stride)):
-        if t is not None:
-            si[:], so[:] = t.stride()[:3], o.stride()[:3]
-    sh.pos_stride[:] = (ps[0] if lead else 0, ps[-2] if positions.dim() == len(lead) + 2 else 0,
-                        ps[-1])
+                         f"(got {list(shape)})")
     if B > 0 and T > 0:
-        _launch("e2s_rotate_positions", (q, k, positions, *outs), _LIB.e2s_rotate_positions,
-                ctypes.byref(sh), ctypes.byref(plan), positions.data_ptr(), _ptr(q), _ptr(k),
-                _ptr(outs[0]), _ptr(outs[1]))
+        sh = _ROTARY.pack(B, T, *heads, _dtype_code(x), 1 if inverse else 0, *strides,
+                          *out_strides, *ps)
+        _launch("e2s_rotate_positions", (q, k, positions, *outs), _LIB.e2s_rotate_positions, sh,
+                ctypes.byref(plan), positions.data_ptr(), ptrs[0], ptrs[2], ptrs[1], ptrs[3])
     return outs[0], outs[1]
 
 
@@ -238,6 +267,7 @@ class PagedCache:
         self.desc = CacheDesc(*k.shape[:1], self.page_tokens, self.num_kv_heads, self.head_dim,
                               st[0], st[1], k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                               v_scale.data_ptr())
+        self.desc_ref = ctypes.byref(self.desc)
 
 
 def cache_append(cache: PagedCache, pages, start, k, v, count=None, src_idx=None,
@@ -248,15 +278,14 @@ def cache_append(cache: PagedCache, pages, start, k, v, count=None, src_idx=None
     keep_idx).  pages [B, max_pages], start and count [B] are int32."""
     torch = _torch()
     G, D = cache.num_kv_heads, cache.head_dim
-    _rows(k, "k")
-    _rows(v, "v", k.dtype)
+    ks = _rows(k, "k")
+    vs = _rows(v, "v", k.dtype)
     B, N = k.shape[0], k.shape[2]
-    if tuple(k.shape) != (B, G, N, D) or v.shape != k.shape:
+    if k.shape != (B, G, N, D) or v.shape != (B, G, N, D):
         raise ValueError(f"k and v must be [B, {G}, N, {D}]")
-    _table(pages, "pages", B)
-    _vector(start, "start", B)
-    if count is not None:
-        _vector(count, "count", B)
+    width, row = _table(pages, "pages", B)
+    start_at = _vector(start, "start", B)
+    count_at = None if count is None else _vector(count, "count", B)
     T = N
     if src_idx is not None:
         _check(src_idx, "src_idx", dtype=torch.int32, ndim=2)
@@ -265,12 +294,10 @@ def cache_append(cache: PagedCache, pages, start, k, v, count=None, src_idx=None
         T = src_idx.shape[1]
     if B == 0 or T == 0:
         return
-    sh = AppendShape(B, T, N, _dtype_code(k), pages.shape[1], 0, pages.stride(0),
-                     (_I64 * 3)(*k.stride()[:3]), (_I64 * 3)(*v.stride()[:3]))
+    sh = _APPEND.pack(B, T, N, _dtype_code(k), width, 0, row, *ks[:3], *vs[:3])
     _launch("e2s_cache_append", (cache.k, pages, start, k, v, count, src_idx),
-            _LIB.e2s_cache_append, ctypes.byref(cache.desc), ctypes.byref(sh), pages.data_ptr(),
-            start.data_ptr(), _ptr(count), _ptr(src_idx), k.data_ptr(), v.data_ptr(),
-            stream=stream)
+            _LIB.e2s_cache_append, cache.desc_ref, sh, pages.data_ptr(), start_at, count_at,
+            _ptr(src_idx), k.data_ptr(), v.data_ptr(), stream=stream)
 
 
 class CacheAttention:
@@ -285,28 +312,30 @@ class CacheAttention:
         self.cache = cache
         self.dtype = torch.bfloat16 if dtype is None else dtype
         code = _dtype_code(torch.empty(0, dtype=self.dtype))
-        self.shape = AttendShape(batch, num_heads, num_queries, code, max_tokens, 1, int(causal),
-                                 int(weights), scale, 0, 1)
         D, G = cache.head_dim, cache.num_kv_heads
+        self.batch, self.max_tokens, self.weights = batch, max_tokens, bool(weights)
         self._q_shape = (batch, num_heads, num_queries, D)
         self._w_shape = (batch, G)
+        self._head = (batch, num_heads, num_queries, code, max_tokens)
+        self._tail = (int(bool(causal)), int(self.weights), float(scale), 0)
         # strides of a dense call: the workspace does not depend on them
-        self.shape.q_stride[:] = (num_heads * num_queries * D, num_queries * D, D)
-        self.shape.out_stride[:] = self.shape.q_stride[:]
-        self.shape.weights_out_stride[:] = (G * max_tokens, max_tokens)
+        rows = (num_heads * num_queries * D, num_queries * D, D)
+        sh = _ATTEND.pack(*self._head, 1, *self._tail, 1, *rows, *rows, G * max_tokens, max_tokens,
+                          G * max_tokens, max_tokens)
         n = ctypes.c_size_t(0)
-        _raise(_LIB.e2s_cache_attend_workspace_size(ctypes.byref(cache.desc),
-                                                    ctypes.byref(self.shape), ctypes.byref(n)),
+        _raise(_LIB.e2s_cache_attend_workspace_size(cache.desc_ref, sh, ctypes.byref(n)),
                "e2s_cache_attend_workspace_size")
         self.workspace = torch.empty(int(n.value), device=cache.device, dtype=torch.uint8)
 
     def _weights(self, t, name):
         torch = _torch()
         _check(t, name, dtype=torch.float32, ndim=3, contiguous=False)
-        if tuple(t.shape[:2]) != self._w_shape or t.shape[2] < self.shape.max_tokens or \
-                (t.stride(2) != 1 and t.shape[2] > 1):
+        st = t.stride()
+        if tuple(t.shape[:2]) != self._w_shape or t.shape[2] < self.max_tokens or \
+                (st[2] != 1 and t.shape[2] > 1):
             raise ValueError(f"{name} must be [{self._w_shape[0]}, {self._w_shape[1]}, >= "
-                             f"{self.shape.max_tokens}] with contiguous rows")
+                             f"{self.max_tokens}] with contiguous rows")
+        return st[:2]
 
     def __call__(self, q, pages, lengths, out=None, q_count=None, weights_in=None,
                  weights_out=None, stream: Optional[int] = None):
@@ -314,40 +343,35 @@ class CacheAttention:
         or None).  See e2s_cache_attend for q_count, weights_in and weights_out; outputs not
         given are allocated, zeros where the call leaves entries as they were."""
         torch = _torch()
-        sh = self.shape
-        if tuple(q.shape) != self._q_shape:
+        qs = _rows(q, "q", self.dtype)
+        if q.shape != self._q_shape:
             raise ValueError(f"q must be {list(self._q_shape)} (got {list(q.shape)})")
-        _rows(q, "q", self.dtype)
-        _table(pages, "pages", sh.batch)
-        _vector(lengths, "lengths", sh.batch)
-        if q_count is not None:
-            _vector(q_count, "q_count", sh.batch)
+        width, row = _table(pages, "pages", self.batch)
+        lengths_at = _vector(lengths, "lengths", self.batch)
+        count_at = None if q_count is None else _vector(q_count, "q_count", self.batch)
         if out is None:
             out = torch.empty_like(q) if q_count is None else torch.zeros_like(q)
+            os_ = out.stride()
         else:
-            _rows(out, "out", self.dtype)
-            if out.shape != q.shape:
+            os_ = _rows(out, "out", self.dtype)
+            if out.shape != self._q_shape:
                 raise ValueError("out must have q's shape")
-        if sh.weights:
+        wi = wo = (0, 0)
+        if self.weights:
             if weights_out is None:
-                weights_out = torch.zeros(self._w_shape + (sh.max_tokens,), device=q.device,
+                weights_out = torch.zeros(self._w_shape + (self.max_tokens,), device=q.device,
                                           dtype=torch.float32)
-            self._weights(weights_out, "weights_out")
-            sh.weights_out_stride[:] = weights_out.stride()[:2]
+            wo = self._weights(weights_out, "weights_out")
             if weights_in is not None:
-                self._weights(weights_in, "weights_in")
-                sh.weights_in_stride[:] = weights_in.stride()[:2]
+                wi = self._weights(weights_in, "weights_in")
         elif weights_in is not None or weights_out is not None:
             raise ValueError("this CacheAttention was made without weights")
-        sh.max_pages, sh.pages_stride = pages.shape[1], pages.stride(0)
-        sh.q_stride[:] = q.stride()[:3]
-        sh.out_stride[:] = out.stride()[:3]
+        sh = _ATTEND.pack(*self._head, width, *self._tail, row, *qs[:3], *os_[:3], *wi, *wo)
         _launch("e2s_cache_attend",
                 (self.workspace, q, pages, lengths, out, q_count, weights_in, weights_out),
-                _LIB.e2s_cache_attend, ctypes.byref(self.cache.desc), ctypes.byref(sh),
-                pages.data_ptr(), lengths.data_ptr(), _ptr(q_count), q.data_ptr(), out.data_ptr(),
-                _ptr(weights_in), _ptr(weights_out), self.workspace.data_ptr(),
-                self.workspace.numel(), stream=stream)
+                _LIB.e2s_cache_attend, self.cache.desc_ref, sh, pages.data_ptr(), lengths_at,
+                count_at, q.data_ptr(), out.data_ptr(), _ptr(weights_in), _ptr(weights_out),
+                self.workspace.data_ptr(), self.workspace.numel(), stream=stream)
         return out, weights_out
 
 
@@ -375,29 +399,30 @@ def cache_evict(cache: PagedCache, pages, lengths, weights, new_pages, budget: i
     weights [B, Hkv, budget] or as given, zeros behind them)."""
     torch = _torch()
     G = cache.num_kv_heads
-    _check(weights, "weights", dtype=torch.float32, ndim=3, contiguous=False)
-    B, N = weights.shape[0], weights.shape[2]
-    if weights.shape[1] != G or (weights.stride(2) != 1 and N > 1):
+    if not (isinstance(weights, torch.Tensor) and weights.is_cuda and
+            weights.dtype is torch.float32 and weights.dim() == 3):
+        _check(weights, "weights", dtype=torch.float32, ndim=3, contiguous=False)
+    (B, g, N), ws = weights.shape, weights.stride()
+    if g != G or (ws[2] != 1 and N > 1):
         raise ValueError(f"weights must be [B, {G}, N] with contiguous rows")
-    _table(pages, "pages", B)
-    _table(new_pages, "new_pages", B)
-    _vector(lengths, "lengths", B)
-    dev = cache.device
-    keep = torch.empty((B, G, max(budget, 0)), device=dev, dtype=torch.int32)
+    width, row = _table(pages, "pages", B)
+    new_width, new_row = _table(new_pages, "new_pages", B)
+    lengths_at = _vector(lengths, "lengths", B)
+    dev, K = cache.device, max(budget, 0)
+    keep = torch.empty((B, G, K), device=dev, dtype=torch.int32)
     kept = torch.empty((B,), device=dev, dtype=torch.int32)
     if weights_left is None:
-        weights_left = torch.empty((B, G, max(budget, 0)), device=dev, dtype=torch.float32)
+        weights_left = torch.empty((B, G, K), device=dev, dtype=torch.float32)
     else:
         _check(weights_left, "weights_left", dtype=torch.float32, ndim=3, contiguous=False)
         if tuple(weights_left.shape[:2]) != (B, G) or \
                 (weights_left.stride(2) != 1 and weights_left.shape[2] > 1):
             raise ValueError(f"weights_left must be [{B}, {G}, >= budget] with contiguous rows")
-    sh = EvictShape(B, N, budget, sinks, recent, pages.shape[1], new_pages.shape[1],
-                    weights_left.shape[2], pages.stride(0), new_pages.stride(0),
-                    (_I64 * 2)(*weights.stride()[:2]), (_I64 * 2)(*weights_left.stride()[:2]))
+    sh = _EVICT.pack(B, N, budget, sinks, recent, width, new_width, weights_left.shape[2], row,
+                     new_row, *ws[:2], *weights_left.stride()[:2])
     _launch("e2s_cache_evict",
             (cache.k, pages, lengths, weights, new_pages, keep, kept, weights_left),
-            _LIB.e2s_cache_evict, ctypes.byref(cache.desc), ctypes.byref(sh), pages.data_ptr(),
-            lengths.data_ptr(), weights.data_ptr(), new_pages.data_ptr(), keep.data_ptr(),
-            kept.data_ptr(), weights_left.data_ptr(), stream=stream)
+            _LIB.e2s_cache_evict, cache.desc_ref, sh, pages.data_ptr(), lengths_at,
+            weights.data_ptr(), new_pages.data_ptr(), keep.data_ptr(), kept.data_ptr(),
+            weights_left.data_ptr(), stream=stream)
     return keep, kept, weights_left

@@ -24,6 +24,8 @@
 // Four waves take neighbouring runs of a workgroup's keys and merge through LDS; the keys
 // of a sequence are split over workgroups when there are too few (sequence, head) pairs to
 // fill the device, and attend_join_kernel joins the parts.
+#include <type_traits>
+
 #include "serve_device.h"
 #include "serve_kernels.h"
 
@@ -60,7 +62,7 @@ struct AttendArgs {
     int64_t logit_stride, chunk;
     int64_t qs[3], os[3], wi[2], wo[2];
     int G, group, T, rows, row_groups, splits;
-    int P, num_pages, max_pages, max_tokens, causal;
+    int P, page_shift, num_pages, max_pages, max_tokens, causal;
     float scale;                     // logit scale times log2(e)
 };
 
@@ -108,35 +110,55 @@ __device__ __forceinline__ bf16x8s widen8(uint32_t a, uint32_t b, float scale) {
                 pack_bf16(b, scale, true)};
     return __builtin_bit_cast(bf16x8s, r);
 }
+template <typename V>
+__device__ __forceinline__ V load_stream(const uint8_t* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+}
 // Words whose bytes are 0x80 where w has a NaN (0x7F or 0xFF).
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
     return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
 }
 
-// The bytes of 32 keys that a wave holds: its part of two 16-key tiles.
+// The permutation of a row's 16-byte chunks in LDS.
+template <int D>
+__device__ __forceinline__ int swizzle(int row) {
+    return D == 128 ? row & 7 : (row >> 1) & 3;
+}
+
+// A wave's part of 32 keys, as loaded.
 template <int D>
 struct Step {
-    u32x4 k[2][D / 64];                  // tile, half of the row
+    u32x4 k[D / 32];                     // 1 KB each of the keys' rows in order
     uint32_t v[8][D / 64];               // key (4 of each tile), words of its D / 16 bytes
 };
 
 template <typename T, int D, int TILES>
-__global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(const AttendArgs a) {
     constexpr int kTerms = Terms<T>::n;
+    constexpr int kParts = kTerms < 2 ? 2 : kTerms;      // bf16 terms of a softmax weight
     constexpr int kHalves = D / 64;
     constexpr int kDims = D / 16;                // dimensions of a lane's values
     constexpr int kPad = D + 4;
-    __shared__ float merge[kAttendWaves][kTile][kPad];
+    constexpr int kFrags = TILES * kTerms * 2 * kHalves;     // operands of the queries
+    // the queries' operands, in the order lanes read them; the waves' outputs at the end
+    __shared__ union {
+        struct {
+            bf16x8s q[kFrags][64];
+            u32x4 k[kAttendWaves][kAttendStep * D / 16];
+        } in;
+        float out[kAttendWaves][kTile][kPad];
+    } lds;
     __shared__ float top_of[kAttendWaves][TILES * kTile], sum_of[kAttendWaves][TILES * kTile];
 
-    int64_t id = blockIdx.x;
-    const int rg = static_cast<int>(id % a.row_groups);
-    id /= a.row_groups;
-    const int split = static_cast<int>(id % a.splits);
-    id /= a.splits;
-    const int g = static_cast<int>(id % a.G);
-    const int64_t b = id / a.G;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t id = blockIdx.x;
+    const int rg = static_cast<int>(id % static_cast<uint32_t>(a.row_groups));
+    id /= static_cast<uint32_t>(a.row_groups);
+    const int split = static_cast<int>(id % static_cast<uint32_t>(a.splits));
+    id /= static_cast<uint32_t>(a.splits);
+    const int g = static_cast<int>(id % static_cast<uint32_t>(a.G));
+    const int64_t b = id / static_cast<uint32_t>(a.G);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g4 = lane >> 4;
 
     const int len = attend_length(a, b), count = attend_count(a, b);
@@ -149,33 +171,108 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
     const int64_t key_begin = split * a.chunk;
     if (split > 0 && key_begin >= most) return;
 
-    // queries as operand columns: lane (n, g4) holds row n's elements 64 h + 16 g4 + 8 s + i
-    bf16x8s q[TILES][kTerms][2 * kHalves];
+    // this wave's keys
+    const int64_t quarter = a.chunk / kAttendWaves;
+    const int w0 = static_cast<int>(min(key_begin + wave * quarter, static_cast<int64_t>(most)));
+    const int w1 = static_cast<int>(min(key_begin + (wave + 1) * quarter,
+                                        static_cast<int64_t>(most)));
+    const int64_t head = static_cast<int64_t>(g) * (D << a.page_shift);
+    const int page_mask = (1 << a.page_shift) - 1;
+
+    // Lane l looks up tile l of 64: its page, or -1, and the block's scales (without a page
+    // any finite scale: the one at hand may not have been written).
+    int page = -1;
+    float ks = 1.0f, vs = 1.0f;
+    auto look_up = [&](int seg) {
+        const int mine = seg + lane * kTile;
+        page = -1;
+        if (mine < w1) page = a.pages[b * a.pages_stride + (mine >> a.page_shift)];
+        if (page >= a.num_pages || page < 0) page = -1;
+        ks = vs = 1.0f;
+        if (page >= 0) {
+            const int64_t at = static_cast<int64_t>(page) * a.G + g;
+            ks = a.k_scale[at];
+            vs = a.v_scale[at];
+        }
+    };
+    // Every address is a uniform base and a lane's constant offset.
+    const uint32_t k_lane = static_cast<uint32_t>(lane * 16);
+    const uint32_t v_lane = static_cast<uint32_t>(4 * g4 * D + n16 * kDims);
+    Step<D> x;
+    auto row_of = [&](int key, int t) { return head + ((key + t * kTile) & page_mask) * D; };
+    // The next step's loads are issued unconditionally, so that a wait counts on them; where
+    // there is no next step (`live` 0) all lanes read the cache's first bytes.
+    auto fetch_k = [&](int key, int seg, uint32_t live) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int i = ((key - seg) >> 4) + t;
+            const int64_t pg = max(__builtin_amdgcn_readlane(page, i), 0);
+            const uint8_t* p = a.k + (live ? pg * a.k_page + row_of(key, t) : 0);
+            const uint32_t at = live ? k_lane : 0;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+                x.k[t * kHalves + h] = load_stream<u32x4>(p + at + h * 1024);
+        }
+    };
+    auto fetch_v = [&](int key, int seg, uint32_t live) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int i = ((key - seg) >> 4) + t;
+            const int64_t pg = max(__builtin_amdgcn_readlane(page, i), 0);
+            const uint8_t* p = a.v + (live ? pg * a.v_page + row_of(key, t) : 0);
+            const uint32_t at = live ? v_lane : 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (kHalves == 2) {
+                    const u32x2 w = load_stream<u32x2>(p + at + r * D);
+                    x.v[4 * t + r][0] = w.x;
+                    x.v[4 * t + r][kHalves - 1] = w.y;
+                } else {
+                    x.v[4 * t + r][0] = load_stream<uint32_t>(p + at + r * D);
+                }
+            }
+        }
+    };
+    if (w0 < w1) {
+        look_up(w0);
+        fetch_k(w0, w0, 1);
+        fetch_v(w0, w0, 1);
+    }
+
+    // Queries as operand columns: lane (n, g4) of an operand holds row n's elements
+    // 64 h + 16 g4 + 8 s + i.  They lie in LDS - in registers they would cost 16 to 48 of
+    // the 128 that leave room for four workgroups on a compute unit - and are read once a
+    // step; each thread lays out operands of its own lane.
     int limit[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
         const int row = row0 + t * kTile + n16;
-        const bool live = row < row_end;
-        const int at = live ? row / a.group : 0;
         // rows that do not exist see everything, so that they mask nothing
-        limit[t] = live ? seen_by(a, len, count, at) : a.max_tokens;
-        const T* src = static_cast<const T*>(a.q) + b * a.qs[0] +
-                       (g * a.group + (live ? row - at * a.group : 0)) * a.qs[1] + at * a.qs[2];
-#pragma unroll
-        for (int s = 0; s < 2 * kHalves; ++s) {
-            Packet<T> p{};
-            if (live) load_packet(p, src + (s >> 1) * 64 + g4 * 16 + (s & 1) * 8);
-            float x[8];
-            unpack(p, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                __bf16 w[kTerms];
-                split_bf16<kTerms>(x[i], w);
-#pragma unroll
-                for (int m = 0; m < kTerms; ++m) q[t][m][s][i] = w[m];
-            }
-        }
+        limit[t] = row < row_end ? seen_by(a, len, count, row / a.group) : a.max_tokens;
     }
+    for (int e = wave; e < TILES * 2 * kHalves; e += kAttendWaves) {
+        const int t = e / (2 * kHalves), s = e - t * (2 * kHalves);
+        const int row = row0 + t * kTile + n16;
+        const int at = row / a.group;
+        Packet<T> p{};
+        if (row < row_end)
+            load_packet(p, static_cast<const T*>(a.q) + b * a.qs[0] +
+                               (g * a.group + row - at * a.group) * a.qs[1] + at * a.qs[2] +
+                               (s >> 1) * 64 + g4 * 16 + (s & 1) * 8);
+        float f[8];
+        unpack(p, f);
+        bf16x8s w[kTerms];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __bf16 part[kTerms];
+            split_bf16<kTerms>(f[i], part);
+#pragma unroll
+            for (int m = 0; m < kTerms; ++m) w[m][i] = part[m];
+        }
+#pragma unroll
+        for (int m = 0; m < kTerms; ++m) lds.in.q[(t * kTerms + m) * 2 * kHalves + s][lane] = w[m];
+    }
+    __syncthreads();
 
     f32x4 o[TILES][kDims];
     float top[TILES], base[TILES], sum[TILES];   // running maximum; the same, 0 before any
@@ -188,189 +285,172 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
         sum[t] = 0.0f;
     }
 
-    // this wave's keys
-    const int64_t quarter = a.chunk / kAttendWaves;
-    const int w0 = static_cast<int>(min(key_begin + wave * quarter, static_cast<int64_t>(most)));
-    const int w1 = static_cast<int>(min(key_begin + (wave + 1) * quarter,
-                                        static_cast<int64_t>(most)));
-    const uint32_t k_lane = static_cast<uint32_t>(n16 * D + g4 * 16);
-    const uint32_t v_lane = static_cast<uint32_t>(4 * g4 * D + n16 * kDims);
-    const int64_t head = static_cast<int64_t>(g) * a.P * D;
+    // One step of 32 keys.  `whole`: every row sees every key of it.
+    auto step = [&](auto whole_tag, int key, int seg, int end) {
+        constexpr bool kWhole = decltype(whole_tag)::value;
+        const int i0 = (key - seg) >> 4;
+        const float ks0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), i0));
+        const float ks1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), i0 + 1));
+        const float vs0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), i0));
+        const float vs1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), i0 + 1));
+        int end0 = 0, end1 = 0;                  // first key of a tile that no page holds
+        if constexpr (!kWhole) {
+            end0 = __builtin_amdgcn_readlane(page, i0) >= 0 ? most : key;
+            end1 = __builtin_amdgcn_readlane(page, i0 + 1) >= 0 ? most : key;
+        }
 
-    for (int seg = w0; seg < w1; seg += 64 * kTile) {
-        // lane l looks up tile l of the next 64: its page, or -1, and the block's scales
-        const int mine = seg + lane * kTile;
-        int page = -1;
-        if (mine < w1) page = a.pages[b * a.pages_stride + mine / a.P];
-        if (page < 0 || page >= a.num_pages) page = -1;
-        const int64_t at = static_cast<int64_t>(max(page, 0)) * a.G + g;
-        // (without a page: any finite scale, the scale at hand may not have been written)
-        const float ks = page < 0 ? 1.0f : a.k_scale[at], vs = page < 0 ? 1.0f : a.v_scale[at];
-        const int seg_end = min(w1, seg + 64 * kTile);
-
-        auto fetch = [&](int key, Step<D>& x) {
+        // The keys' rows go through the wave's own part of LDS into operand order (16 bytes
+        // of one row per lane, 16 rows side by side).  A row's 16-byte chunks are permuted by
+        // its number, so that neighbouring rows' equal chunks lie in different banks.  A
+        // wave's LDS accesses keep their order, so nothing waits.
+        constexpr int kChunks = D / 16;
+        u32x4* const mine = lds.in.k[wave];
+#pragma unroll
+        for (int j = 0; j < 2 * kHalves; ++j) {
+            const int r = (j * 64 + lane) / kChunks, c = lane % kChunks;
+            mine[r * kChunks + (c ^ swizzle<D>(r))] = x.k[j];
+        }
+        // an index that the compiler cannot know keeps the reads of the queries in the loop,
+        // and their registers free
+        int my = lane;
+        asm volatile("" : "+v"(my));
+        f32x4 s[TILES][2];
+#pragma unroll
+        for (int u = 0; u < TILES; ++u)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) s[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+            u32x4 w[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const int i = (key - seg) / kTile + t;
-                const int pg = max(__builtin_amdgcn_readlane(page, i), 0);
-                const int64_t row = head + static_cast<int64_t>((key + t * kTile) % a.P) * D;
-                const uint8_t* kp = a.k + pg * a.k_page + row;
-                const uint8_t* vp = a.v + pg * a.v_page + row;
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h)
-                    x.k[t][h] = __builtin_nontemporal_load(
-                        reinterpret_cast<const u32x4*>(kp + k_lane + h * 64));
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint8_t* p = vp + v_lane + r * D;
-                    if constexpr (kHalves == 2) {
-                        const u32x2 w = __builtin_nontemporal_load(
-                            reinterpret_cast<const u32x2*>(p));
-                        x.v[4 * t + r][0] = w.x;
-                        x.v[4 * t + r][kHalves - 1] = w.y;
-                    } else {
-                        x.v[4 * t + r][0] = __builtin_nontemporal_load(
-                            reinterpret_cast<const uint32_t*>(p));
-                    }
-                }
+                const int r = t * kTile + n16;
+                w[t] = mine[r * kChunks + ((4 * h + g4) ^ swizzle<D>(r))];
             }
-        };
-
-        Step<D> cur, next;
-        fetch(seg, cur);
-        for (int key = seg; key < seg_end; key += kAttendStep) {
-            if (key + kAttendStep < seg_end) fetch(key + kAttendStep, next);
-            const int i0 = (key - seg) / kTile;
-            const int pg0 = __builtin_amdgcn_readlane(page, i0);
-            const int pg1 = __builtin_amdgcn_readlane(page, i0 + 1);
-            const float ks0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), i0));
-            const float ks1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), i0 + 1));
-            const float vs0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), i0));
-            const float vs1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), i0 + 1));
-
-            // S^T of both tiles
-            f32x4 s[TILES][2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const float sc = t ? ks1 : ks0;
-                bf16x8s kf[2 * kHalves];
+            for (int e = 0; e < 2; ++e) {
+                bf16x8s kf[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    kf[t] = e ? widen8(w[t].z, w[t].w, t ? ks1 : ks0)
+                              : widen8(w[t].x, w[t].y, t ? ks1 : ks0);
+#pragma unroll
+                for (int u = 0; u < TILES; ++u)
+#pragma unroll
+                    for (int m = kTerms - 1; m >= 0; --m) {
+                        const bf16x8s qf = lds.in.q[(u * kTerms + m) * 2 * kHalves + 2 * h + e][my];
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            s[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t], qf, s[u][t],
+                                                                              0, 0, 0);
+                    }
+            }
+        }
+        const uint32_t live = key + kAttendStep < end;
+        const int next = live ? key + kAttendStep : key;
+        fetch_k(next, seg, live);
+
+        bool lost = false;                       // a NaN among the values of a masked step
+        if constexpr (!kWhole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int kk = key + (i >> 2) * kTile + 4 * g4 + (i & 3);
+                const bool there = kk < ((i >> 2) ? end1 : end0);
 #pragma unroll
                 for (int h = 0; h < kHalves; ++h) {
-                    kf[2 * h] = widen8(cur.k[t][h].x, cur.k[t][h].y, sc);
-                    kf[2 * h + 1] = widen8(cur.k[t][h].z, cur.k[t][h].w, sc);
-                }
-#pragma unroll
-                for (int u = 0; u < TILES; ++u) {
-                    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int m = kTerms - 1; m >= 0; --m)
-#pragma unroll
-                        for (int e = 0; e < 2 * kHalves; ++e)
-                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[e], q[u][m][e], acc,
-                                                                          0, 0, 0);
-                    s[u][t] = acc;
+                    // what no row sees may hold anything: 0 * NaN must not reach the sum
+                    if (!there) x.v[i][h] = 0u;
+                    lost = lost || nan_bytes(x.v[i][h]) != 0u;
                 }
             }
-            // keys that some row does not see: beyond `least`, or without a page
-            const bool whole = key + kAttendStep <= least && pg0 >= 0 && pg1 >= 0;
-            bool lost = false;                   // a NaN among the values of a masked step
-            if (!whole) {
+            lost = __ballot(lost) != 0;
+        }
+        bf16x8s pf[TILES][kParts];               // weights as operand columns, in parts
+#pragma unroll
+        for (int u = 0; u < TILES; ++u) {
+            float y[8];                          // logits before their scale
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = s[u][i >> 2][i & 3];
+            if constexpr (!kWhole) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int kk = key + (i >> 2) * kTile + 4 * g4 + (i & 3);
-                    const bool there = kk < most && ((i >> 2) ? pg1 : pg0) >= 0;
-#pragma unroll
-                    for (int h = 0; h < kHalves; ++h) {
-                        // what no row sees may hold anything: 0 * NaN must not reach the sum
-                        if (!there) cur.v[i][h] = 0u;
-                        lost = lost || nan_bytes(cur.v[i][h]) != 0u;
-                    }
+                    if (kk >= min(limit[u], (i >> 2) ? end1 : end0)) y[i] = -kInf;
                 }
-                lost = __ballot(lost) != 0;
             }
-#pragma unroll
-            for (int u = 0; u < TILES; ++u) {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = s[u][i >> 2][i & 3] * a.scale;
-                if (!whole) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int kk = key + (i >> 2) * kTile + 4 * g4 + (i & 3);
-                        if (kk >= limit[u] || ((i >> 2) ? pg1 : pg0) < 0)
-                            x[i] = -kInf;
-                    }
+            if (a.logits) {
+                // a uniform base and a lane's offset, which is not worth a register
+                const int row = row0 + u * kTile + (my & 15);
+                float* to = a.logits +
+                            ((b * a.G + g) * static_cast<int64_t>(a.rows) + row0 + u * kTile) *
+                                a.logit_stride + key;
+                const uint32_t at = static_cast<uint32_t>(my & 15) *
+                                        static_cast<uint32_t>(a.logit_stride) + (my >> 4) * 4;
+                if (row < row_end) {
+                    *reinterpret_cast<f32x4*>(to + at) =
+                        f32x4{y[0] * a.scale, y[1] * a.scale, y[2] * a.scale, y[3] * a.scale};
+                    *reinterpret_cast<f32x4*>(to + at + kTile) =
+                        f32x4{y[4] * a.scale, y[5] * a.scale, y[6] * a.scale, y[7] * a.scale};
                 }
-                if (a.logits) {
-                    const int row = row0 + u * kTile + n16;
-                    if (row < row_end) {
-                        float* to = a.logits +
-                                    ((b * a.G + g) * static_cast<int64_t>(a.rows) + row) *
-                                        a.logit_stride + key + 4 * g4;
-                        *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
-                        *reinterpret_cast<f32x4*>(to + kTile) = f32x4{x[4], x[5], x[6], x[7]};
-                    }
-                }
-                float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                                 fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-                if (__ballot(mx > top[u] + kRaise)) {
-                    mx = fmaxf(mx, __shfl_xor(mx, 16));
-                    mx = fmaxf(mx, __shfl_xor(mx, 32));
-                    const float up = fmaxf(top[u], mx);
-                    const float shrink = up == top[u] ? 1.0f : exp2_hw(top[u] - up);
-                    top[u] = up;
-                    base[u] = up == -kInf ? 0.0f : up;
-                    sum[u] *= shrink;
-#pragma unroll
-                    for (int j = 0; j < kDims; ++j) o[u][j] *= shrink;
-                }
-                float p[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = exp2_hw(x[i] - base[u]);
-                sum[u] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[u][i >> 2][i & 3] = p[i];
             }
-            // weights as operand columns, in kTerms parts
-            bf16x8s pf[TILES][kTerms];
+            // (the scale is positive)
+            float mx = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])),
+                             fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7]))) * a.scale;
+            if (__ballot(mx > top[u] + kRaise)) {
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float up = fmaxf(top[u], mx);
+                const float shrink = up == top[u] ? 1.0f : exp2_hw(top[u] - up);
+                top[u] = up;
+                base[u] = up == -kInf ? 0.0f : up;
+                sum[u] *= shrink;
 #pragma unroll
-            for (int u = 0; u < TILES; ++u)
+                for (int j = 0; j < kDims; ++j) o[u][j] *= shrink;
+            }
+            float p[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    __bf16 w[kTerms];
-                    split_bf16<kTerms>(s[u][i >> 2][i & 3], w);
+            for (int i = 0; i < 8; ++i) p[i] = exp2_hw(__builtin_fmaf(y[i], a.scale, -base[u]));
+            sum[u] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma unroll
-                    for (int m = 0; m < kTerms; ++m) pf[u][m][i] = w[m];
-                }
-            // O^T: 4 dimensions of each word, keys paired by byte permutation
+            for (int i = 0; i < 8; ++i) {
+                __bf16 w[kParts];
+                split_bf16<kParts>(p[i], w);
 #pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                u32x4s vf[4];
+                for (int m = 0; m < kParts; ++m) pf[u][m][i] = w[m];
+            }
+        }
+        // O^T: 4 dimensions of each word, keys paired by byte permutation
 #pragma unroll
-                for (int pr = 0; pr < 4; ++pr) {
-                    uint32_t wa = cur.v[2 * pr][h], wb = cur.v[2 * pr + 1][h];
+        for (int h = 0; h < kHalves; ++h) {
+            u32x4s vf[4];
+#pragma unroll
+            for (int pr = 0; pr < 4; ++pr) {
+                uint32_t wa = x.v[2 * pr][h], wb = x.v[2 * pr + 1][h];
+                if constexpr (!kWhole) {
                     if (lost) {                  // NaN bytes to 0 here, counted below
                         wa &= ~((nan_bytes(wa) >> 7) * 0xFFu);
                         wb &= ~((nan_bytes(wb) >> 7) * 0xFFu);
                     }
-                    const uint32_t lo = __builtin_amdgcn_perm(wb, wa, 0x05010400u);
-                    const uint32_t hi = __builtin_amdgcn_perm(wb, wa, 0x07030602u);
-                    const float sc = pr < 2 ? vs0 : vs1;
-                    vf[0][pr] = pack_bf16(lo, sc, false);
-                    vf[1][pr] = pack_bf16(lo, sc, true);
-                    vf[2][pr] = pack_bf16(hi, sc, false);
-                    vf[3][pr] = pack_bf16(hi, sc, true);
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int u = 0; u < TILES; ++u)
-#pragma unroll
-                        for (int m = kTerms - 1; m >= 0; --m)
-                            o[u][4 * h + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                __builtin_bit_cast(bf16x8s, vf[j]), pf[u][m], o[u][4 * h + j], 0,
-                                0, 0);
+                const uint32_t lo = __builtin_amdgcn_perm(wb, wa, 0x05010400u);
+                const uint32_t hi = __builtin_amdgcn_perm(wb, wa, 0x07030602u);
+                const float sc = pr < 2 ? vs0 : vs1;
+                vf[0][pr] = pack_bf16(lo, sc, false);
+                vf[1][pr] = pack_bf16(lo, sc, true);
+                vf[2][pr] = pack_bf16(hi, sc, false);
+                vf[3][pr] = pack_bf16(hi, sc, true);
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int u = 0; u < TILES; ++u)
+#pragma unroll
+                    for (int m = kParts - 1; m >= 0; --m)
+                        o[u][4 * h + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8s, vf[j]), pf[u][m], o[u][4 * h + j], 0, 0,
+                            0);
+        }
+        if constexpr (!kWhole) {
             if (lost) {
                 // A NaN value reaches the rows that see its key, and no other: count, per
                 // dimension and row, the seen keys that hold one.
@@ -388,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         bad[i] = static_cast<__bf16>(
-                            (nan_bytes(cur.v[i][j / 4]) >> (8 * (j % 4) + 7)) & 1u ? 1.0f : 0.0f);
+                            (nan_bytes(x.v[i][j / 4]) >> (8 * (j % 4) + 7)) & 1u ? 1.0f : 0.0f);
 #pragma unroll
                     for (int u = 0; u < TILES; ++u) {
                         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -400,11 +480,29 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
                     }
                 }
             }
-            cur = next;
         }
+        fetch_v(next, seg, live);
+    };
+
+    for (int seg = w0; seg < w1; seg += 64 * kTile) {
+        const int seg_end = min(w1, seg + 64 * kTile);
+        if (seg > w0) {
+            look_up(seg);
+            fetch_k(seg, seg, 1);
+            fetch_v(seg, seg, 1);
+        }
+        // steps that every row sees whole: before `least`, if all of the segment's pages exist
+        const bool paged = __ballot(seg + lane * kTile < seg_end && page < 0) == 0;
+        const int whole_end = paged ? min(seg_end, least) : seg;
+        int key = seg;
+        for (; key + kAttendStep <= whole_end; key += kAttendStep)
+            step(std::true_type{}, key, seg, seg_end);
+        for (; key < seg_end; key += kAttendStep)
+            step(std::false_type{}, key, seg, seg_end);
     }
 
-    // merge the four waves, a 16-row tile at a time
+    // merge the four waves, a 16-row tile at a time (all have read their last queries)
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
         sum[u] += __shfl_xor(sum[u], 16);
@@ -420,15 +518,13 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
         float all = top_of[0][u * kTile + n16];
 #pragma unroll
         for (int w = 1; w < kAttendWaves; ++w) all = fmaxf(all, top_of[w][u * kTile + n16]);
-        const float f = top[u] == -kInf ? 0.0f
-                        : top[u] == all                  ? 1.0f
-                                                         : exp2_hw(top[u] - all);
+        const float f = top[u] == -kInf ? 0.0f : top[u] == all ? 1.0f : exp2_hw(top[u] - all);
         // lane (n, g4) holds dimensions (4 g4 + r) * kDims + j of row n
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int j = 0; j < kDims; ++j)
-                merge[wave][n16][(4 * g4 + r) * kDims + j] = o[u][j][r] * f;
+                lds.out[wave][n16][(4 * g4 + r) * kDims + j] = o[u][j][r] * f;
         __syncthreads();
         constexpr int kPer = kTile * D / kThreads;       // dimensions per thread: 4 or 8
         const int r = threadIdx.x / (D / kPer), d0 = threadIdx.x % (D / kPer) * kPer;
@@ -448,9 +544,9 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
             float y[kPer];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                y[i] = merge[0][r][d0 + i];
+                y[i] = lds.out[0][r][d0 + i];
 #pragma unroll
-                for (int w = 1; w < kAttendWaves; ++w) y[i] += merge[w][r][d0 + i];
+                for (int w = 1; w < kAttendWaves; ++w) y[i] += lds.out[w][r][d0 + i];
             }
             const int64_t line = (b * a.G + g) * static_cast<int64_t>(a.rows) + row;
             if (a.splits == 1) {
@@ -463,8 +559,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(const AttendArgs a) {
                 for (int i = 0; i < kPer; ++i) z.x[i] = from_f32<T>(y[i] * inv);
                 *reinterpret_cast<Run<T, kPer>*>(to) = z;
                 if (a.lse && d0 == 0)
-                    a.lse[line] = total > 0.0f || total != total ? m + __log2f(total)
-                                                                 : -kInf;
+                    a.lse[line] = total > 0.0f || total != total ? m + __log2f(total) : -kInf;
             } else {
                 const int64_t part = line * a.splits + split;
                 Run<float, kPer> z;
@@ -639,6 +734,7 @@ hipError_t launch_cache_attend(const e2s_cache& c, const e2s_cache_attend_shape&
     a.row_groups = static_cast<int>(p.row_groups);
     a.splits = static_cast<int>(p.splits);
     a.P = c.page_tokens;
+    a.page_shift = __builtin_ctz(static_cast<unsigned>(c.page_tokens));   // a power of two
     a.num_pages = c.num_pages;
     a.max_pages = s.max_pages;
     a.max_tokens = s.max_tokens;

@@ -251,7 +251,7 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     p.row_groups = (p.rows + 16 * p.tiles - 1) / (16 * p.tiles);
     const int64_t unit = kAttendStep * kAttendWaves;
     const int64_t units = B * G * p.row_groups;
-    const int64_t want = 1536;      // workgroups that fill the device several times over
+    const int64_t want = 2048;      // workgroups that fill the device several times over
     int64_t per = (s.max_tokens * units + want - 1) / want;
     per = std::max<int64_t>(per, 2 * unit);
     p.chunk = (per + unit - 1) / unit * unit;
