@@ -408,11 +408,10 @@ def cache_evict(cache: PagedCache, pages, lengths, weights, new_pages, budget: i
     width, row = _table(pages, "pages", B)
     new_width, new_row = _table(new_pages, "new_pages", B)
     lengths_at = _vector(lengths, "lengths", B)
-    dev, K = cache.device, max(budget, 0)
-    keep = torch.empty((B, G, K), device=dev, dtype=torch.int32)
-    kept = torch.empty((B,), device=dev, dtype=torch.int32)
+    K = max(budget, 0)
+    keep, kept = lengths.new_empty((B, G, K)), torch.empty_like(lengths)
     if weights_left is None:
-        weights_left = torch.empty((B, G, K), device=dev, dtype=torch.float32)
+        weights_left = weights.new_empty((B, G, K))
     else:
         _check(weights_left, "weights_left", dtype=torch.float32, ndim=3, contiguous=False)
         if tuple(weights_left.shape[:2]) != (B, G) or \

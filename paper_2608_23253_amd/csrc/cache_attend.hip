@@ -110,6 +110,12 @@ __device__ __forceinline__ bf16x8s widen8(uint32_t a, uint32_t b, float scale) {
                 pack_bf16(b, scale, true)};
     return __builtin_bit_cast(bf16x8s, r);
 }
+// What the wave's lanes wrote to LDS before is what they read after, and the other way round:
+// the hardware keeps a wave's accesses in order, this keeps the compiler's.
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 template <typename V>
 __device__ __forceinline__ V load_stream(const uint8_t* p) {
     return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
@@ -117,6 +123,61 @@ __device__ __forceinline__ V load_stream(const uint8_t* p) {
 // Words whose bytes are 0x80 where w has a NaN (0x7F or 0xFF).
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
     return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+}
+
+// Logits (before their positive scale, -inf where masked) to weights against a row's running
+// maximum, which is raised - with the sum and the output so far - where a logit passes it by
+// more than kRaise.  The four lanes of a row hold N of its logits each, and part of its sum.
+template <int N, int DIMS>
+__device__ __forceinline__ void weigh(float (&y)[N], float scale, float& top, float& base,
+                                      float& sum, f32x4 (&o)[DIMS]) {
+    float mx = fmaxf(y[0], y[1]);
+#pragma unroll
+    for (int i = 2; i < N; i += 2) mx = fmaxf(mx, fmaxf(y[i], y[i + 1]));
+    mx *= scale;
+    if (__ballot(mx > top + kRaise)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float up = fmaxf(top, mx);
+        const float shrink = up == top ? 1.0f : exp2_hw(top - up);
+        top = up;
+        base = up == -kInf ? 0.0f : up;
+        sum *= shrink;
+#pragma unroll
+        for (int j = 0; j < DIMS; ++j) o[j] *= shrink;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = exp2_hw(__builtin_fmaf(y[i], scale, -base));
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        sum += ((y[i] + y[i + 1]) + (y[i + 2] + y[i + 3])) +
+               ((y[i + 4] + y[i + 5]) + (y[i + 6] + y[i + 7]));
+}
+
+// The weight that tokens n0 .. n0 + 3, n0 + step .. received: the sum over the rows, in
+// order, of exp2(logit - lse), from the stored logits.  lse: per row, -inf where it sees none.
+__device__ __forceinline__ void token_weights(const AttendArgs& a, int64_t b, int g,
+                                              const float* lse, int len, int count, int n0,
+                                              int step) {
+    const int64_t bg = b * a.G + g;
+    const int rows = count * a.group;
+    const float* in = a.w_in ? a.w_in + b * a.wi[0] + g * a.wi[1] : nullptr;
+    float* out = a.w_out + b * a.wo[0] + g * a.wo[1];
+    for (; n0 < len; n0 += step) {
+        float w[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int row = 0; row < rows; ++row) {
+            const int limit = seen_by(a, len, count, row / a.group);
+            const float l = lse[row];
+            if (n0 >= limit || l == -kInf) continue;
+            const f32x4 x = *reinterpret_cast<const f32x4*>(
+                a.logits + (bg * a.rows + row) * a.logit_stride + n0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] += n0 + i < limit ? exp2_hw(x[i] - l) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n0 + i < len) out[n0 + i] = in ? in[n0 + i] + w[i] : w[i];
+    }
 }
 
 // The permutation of a row's 16-byte chunks in LDS.
@@ -132,8 +193,9 @@ struct Step {
     uint32_t v[8][D / 64];               // key (4 of each tile), words of its D / 16 bytes
 };
 
-template <typename T, int D, int TILES>
-__global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(const AttendArgs a) {
+template <typename T, int D, int TILES, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, TILES == 1 && WAVES == 4 ? 3 : 2) void attend_kernel(
+    const AttendArgs a) {
     constexpr int kTerms = Terms<T>::n;
     constexpr int kParts = kTerms < 2 ? 2 : kTerms;      // bf16 terms of a softmax weight
     constexpr int kHalves = D / 64;
@@ -144,15 +206,15 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
     __shared__ union {
         struct {
             bf16x8s q[kFrags][64];
-            u32x4 k[kAttendWaves][kAttendStep * D / 16];
+            u32x4 k[WAVES][kAttendStep * D / 16];
         } in;
-        float out[kAttendWaves][kTile][kPad];
+        float out[WAVES][kTile][kPad];
     } lds;
-    __shared__ float top_of[kAttendWaves][TILES * kTile], sum_of[kAttendWaves][TILES * kTile];
+    __shared__ float top_of[WAVES][TILES * kTile], sum_of[WAVES][TILES * kTile];
+
+    __shared__ float lse_of[TILES * kTile];
 
     uint32_t id = blockIdx.x;
-    const int rg = static_cast<int>(id % static_cast<uint32_t>(a.row_groups));
-    id /= static_cast<uint32_t>(a.row_groups);
     const int split = static_cast<int>(id % static_cast<uint32_t>(a.splits));
     id /= static_cast<uint32_t>(a.splits);
     const int g = static_cast<int>(id % static_cast<uint32_t>(a.G));
@@ -161,33 +223,38 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g4 = lane >> 4;
 
+    // Lane l looks up tile l of 64: its page, or -1, and the block's scales (without a page
+    // any finite scale: the one at hand may not have been written).  The first lookup does
+    // not wait for the length.
+    const int64_t key_begin = split * a.chunk, quarter = a.chunk / WAVES;
+    const int64_t cap = static_cast<int64_t>(a.max_pages) << a.page_shift;
+    const int64_t wave_begin = key_begin + wave * quarter;
+    auto page_at = [&](int64_t key, int64_t end) {
+        return key < end ? a.pages[b * a.pages_stride + (key >> a.page_shift)] : -1;
+    };
+    int page = page_at(wave_begin + lane * kTile, min(wave_begin + quarter, cap));
+
     const int len = attend_length(a, b), count = attend_count(a, b);
-    const int row0 = rg * TILES * kTile;
-    const int row_end = min(row0 + TILES * kTile, count * a.group);
-    if (row0 >= row_end) return;
-    // what the workgroup's first row and last row see: every row sees between them
-    const int least = seen_by(a, len, count, row0 / a.group);
-    const int most = seen_by(a, len, count, (row_end - 1) / a.group);
-    const int64_t key_begin = split * a.chunk;
+    constexpr int row0 = 0;
+    const int row_end = count * a.group;
+    if (row_end == 0) {                          // no query: no weight is added
+        if (WAVES == 8 && a.w_out)
+            token_weights(a, b, g, lse_of, len, 0, static_cast<int>(threadIdx.x) * 4, 256 * WAVES);
+        return;
+    }
+    // what the first row and the last row see: every row sees between them
+    const int least = seen_by(a, len, count, 0);
+    const int most = seen_by(a, len, count, count - 1);
     if (split > 0 && key_begin >= most) return;
 
     // this wave's keys
-    const int64_t quarter = a.chunk / kAttendWaves;
-    const int w0 = static_cast<int>(min(key_begin + wave * quarter, static_cast<int64_t>(most)));
-    const int w1 = static_cast<int>(min(key_begin + (wave + 1) * quarter,
-                                        static_cast<int64_t>(most)));
+    const int w0 = static_cast<int>(min(wave_begin, static_cast<int64_t>(most)));
+    const int w1 = static_cast<int>(min(wave_begin + quarter, static_cast<int64_t>(most)));
     const int64_t head = static_cast<int64_t>(g) * (D << a.page_shift);
     const int page_mask = (1 << a.page_shift) - 1;
-
-    // Lane l looks up tile l of 64: its page, or -1, and the block's scales (without a page
-    // any finite scale: the one at hand may not have been written).
-    int page = -1;
     float ks = 1.0f, vs = 1.0f;
     auto look_up = [&](int seg) {
-        const int mine = seg + lane * kTile;
-        page = -1;
-        if (mine < w1) page = a.pages[b * a.pages_stride + (mine >> a.page_shift)];
-        if (page >= a.num_pages || page < 0) page = -1;
+        if (seg + lane * kTile >= w1 || page >= a.num_pages || page < 0) page = -1;
         ks = vs = 1.0f;
         if (page >= 0) {
             const int64_t at = static_cast<int64_t>(page) * a.G + g;
@@ -250,7 +317,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
         // rows that do not exist see everything, so that they mask nothing
         limit[t] = row < row_end ? seen_by(a, len, count, row / a.group) : a.max_tokens;
     }
-    for (int e = wave; e < TILES * 2 * kHalves; e += kAttendWaves) {
+    for (int e = wave; e < TILES * 2 * kHalves; e += WAVES) {
         const int t = e / (2 * kHalves), s = e - t * (2 * kHalves);
         const int row = row0 + t * kTile + n16;
         const int at = row / a.group;
@@ -310,6 +377,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
             const int r = (j * 64 + lane) / kChunks, c = lane % kChunks;
             mine[r * kChunks + (c ^ swizzle<D>(r))] = x.k[j];
         }
+        wave_order();
         // an index that the compiler cannot know keeps the reads of the queries in the loop,
         // and their registers free
         int my = lane;
@@ -346,6 +414,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
                     }
             }
         }
+        wave_order();
         const uint32_t live = key + kAttendStep < end;
         const int next = live ? key + kAttendStep : key;
         fetch_k(next, seg, live);
@@ -393,28 +462,11 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
                         f32x4{y[4] * a.scale, y[5] * a.scale, y[6] * a.scale, y[7] * a.scale};
                 }
             }
-            // (the scale is positive)
-            float mx = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])),
-                             fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7]))) * a.scale;
-            if (__ballot(mx > top[u] + kRaise)) {
-                mx = fmaxf(mx, __shfl_xor(mx, 16));
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float up = fmaxf(top[u], mx);
-                const float shrink = up == top[u] ? 1.0f : exp2_hw(top[u] - up);
-                top[u] = up;
-                base[u] = up == -kInf ? 0.0f : up;
-                sum[u] *= shrink;
-#pragma unroll
-                for (int j = 0; j < kDims; ++j) o[u][j] *= shrink;
-            }
-            float p[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = exp2_hw(__builtin_fmaf(y[i], a.scale, -base[u]));
-            sum[u] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+            weigh<8, kDims>(y, a.scale, top[u], base[u], sum[u], o[u]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 __bf16 w[kParts];
-                split_bf16<kParts>(p[i], w);
+                split_bf16<kParts>(y[i], w);
 #pragma unroll
                 for (int m = 0; m < kParts; ++m) pf[u][m][i] = w[m];
             }
@@ -487,6 +539,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
     for (int seg = w0; seg < w1; seg += 64 * kTile) {
         const int seg_end = min(w1, seg + 64 * kTile);
         if (seg > w0) {
+            page = page_at(seg + lane * kTile, w1);
             look_up(seg);
             fetch_k(seg, seg, 1);
             fetch_v(seg, seg, 1);
@@ -517,7 +570,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
     for (int u = 0; u < TILES; ++u) {
         float all = top_of[0][u * kTile + n16];
 #pragma unroll
-        for (int w = 1; w < kAttendWaves; ++w) all = fmaxf(all, top_of[w][u * kTile + n16]);
+        for (int w = 1; w < WAVES; ++w) all = fmaxf(all, top_of[w][u * kTile + n16]);
         const float f = top[u] == -kInf ? 0.0f : top[u] == all ? 1.0f : exp2_hw(top[u] - all);
         // lane (n, g4) holds dimensions (4 g4 + r) * kDims + j of row n
 #pragma unroll
@@ -526,16 +579,16 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
             for (int j = 0; j < kDims; ++j)
                 lds.out[wave][n16][(4 * g4 + r) * kDims + j] = o[u][j][r] * f;
         __syncthreads();
-        constexpr int kPer = kTile * D / kThreads;       // dimensions per thread: 4 or 8
+        constexpr int kPer = kTile * D / (64 * WAVES);   // dimensions per thread: 2 to 8
         const int r = threadIdx.x / (D / kPer), d0 = threadIdx.x % (D / kPer) * kPer;
         const int row = row0 + u * kTile + r;
         if (row < row_end) {
             float m = top_of[0][u * kTile + r];
 #pragma unroll
-            for (int w = 1; w < kAttendWaves; ++w) m = fmaxf(m, top_of[w][u * kTile + r]);
+            for (int w = 1; w < WAVES; ++w) m = fmaxf(m, top_of[w][u * kTile + r]);
             float total = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kAttendWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 // without a maximum a sum is 0, or NaN, which stays
                 const float tw = top_of[w][u * kTile + r];
                 total += sum_of[w][u * kTile + r] *
@@ -546,7 +599,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
             for (int i = 0; i < kPer; ++i) {
                 y[i] = lds.out[0][r][d0 + i];
 #pragma unroll
-                for (int w = 1; w < kAttendWaves; ++w) y[i] += lds.out[w][r][d0 + i];
+                for (int w = 1; w < WAVES; ++w) y[i] += lds.out[w][r][d0 + i];
             }
             const int64_t line = (b * a.G + g) * static_cast<int64_t>(a.rows) + row;
             if (a.splits == 1) {
@@ -558,8 +611,11 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) z.x[i] = from_f32<T>(y[i] * inv);
                 *reinterpret_cast<Run<T, kPer>*>(to) = z;
-                if (a.lse && d0 == 0)
-                    a.lse[line] = total > 0.0f || total != total ? m + __log2f(total) : -kInf;
+                if (d0 == 0) {
+                    const float l = total > 0.0f || total != total ? m + __log2f(total) : -kInf;
+                    lse_of[u * kTile + r] = l;
+                    if (a.lse) a.lse[line] = l;
+                }
             } else {
                 const int64_t part = line * a.splits + split;
                 Run<float, kPer> z;
@@ -574,33 +630,407 @@ __global__ __launch_bounds__(kThreads, TILES == 1 ? 3 : 2) void attend_kernel(co
         }
         __syncthreads();
     }
+    // A call of few workgroups that see every token turns its logits into weights itself:
+    // they were stored by other waves of the same workgroup, before the barriers above.
+    if (WAVES == 8 && a.w_out)
+        token_weights(a, b, g, lse_of, len, count, static_cast<int>(threadIdx.x) * 4, 256 * WAVES);
 }
 
-// Joins the parts of a row: one workgroup per (sequence, key head, row).  A part is there
-// where its first key is seen by the workgroup that wrote it; parts whose keys this row
-// does not see hold a maximum of -inf.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void attend_join_kernel(const AttendArgs a) {
-    __shared__ float merge[kAttendWaves][D];
-    __shared__ float sums[kAttendWaves];
-    const int64_t line = blockIdx.x;
-    const int64_t bg = line / a.rows;
+// Many rows per key head (a run of queries): attend_rows_kernel.  Here the products count,
+// and every row needs the same widened keys and values, so a workgroup widens 64 keys at a
+// time into LDS, in the order in which operands are read, and its four waves take 16 * TILES
+// rows each over all keys.  Wave w widens 16-key tile w: page and scales are uniform to it.
+// One buffer of 33 KB, so that four workgroups of 16-row waves share a compute unit and one
+// multiplies while another widens or waits: a wave's step is a chain of dependent products,
+// maxima and exponentials that leaves most of its issue slots to others.
+constexpr int kRowStep = 64;
+
+template <int D>
+struct RowsShared {
+    // operand e of tile t, operand j of 32 keys; a key operand's lanes are permuted by its
+    // 16-byte chunk, so that the chunks of one row, written together, lie in different banks
+    bf16x8s k[4][D / 32][64];
+    u32x2 v[2][D / 16][64][2];           // two halves: 8 bytes of each 16-key tile
+    uint8_t nan[4][kTile][16];           // per key, a bit per dimension: masked steps only
+    int state[4];                        // of each tile: kNoPage, kLost
+};
+constexpr int kNoPage = 1, kLost = 2;    // kLost: a NaN among the values (masked steps)
+
+template <typename T, int D, int TILES>
+__global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) void attend_rows_kernel(const AttendArgs a) {
+    constexpr int kTerms = Terms<T>::n;
+    constexpr int kParts = kTerms < 2 ? 2 : kTerms;
+    constexpr int kHalves = D / 64;
+    constexpr int kDims = D / 16;
+    constexpr int kSteps = 2 * kHalves;          // operands along a row
+    constexpr int kChunks = D / 16;
+    __shared__ RowsShared<D> lds;
+
+    uint32_t id = blockIdx.x;
+    const int rg = static_cast<int>(id % static_cast<uint32_t>(a.row_groups));
+    id /= static_cast<uint32_t>(a.row_groups);
+    const int split = static_cast<int>(id % static_cast<uint32_t>(a.splits));
+    id /= static_cast<uint32_t>(a.splits);
+    const int g = static_cast<int>(id % static_cast<uint32_t>(a.G));
+    const int64_t b = id / static_cast<uint32_t>(a.G);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, g4 = lane >> 4;
+
+    const int len = attend_length(a, b), count = attend_count(a, b);
+    const int group0 = rg * TILES * kTile * kAttendWaves;
+    const int group_end = min(group0 + TILES * kTile * kAttendWaves, count * a.group);
+    if (group0 >= group_end) return;
+    const int least = seen_by(a, len, count, group0 / a.group);
+    const int most = seen_by(a, len, count, (group_end - 1) / a.group);
+    const int64_t key_begin = split * a.chunk;
+    if (split > 0 && key_begin >= most) return;
+    const int k0 = static_cast<int>(key_begin);
+    const int k1 = static_cast<int>(min(key_begin + a.chunk, static_cast<int64_t>(most)));
+
+    // this wave's rows
+    const int row0 = group0 + wave * TILES * kTile;
+    const int row_end = min(row0 + TILES * kTile, group_end);
+    int limit[TILES];
+    bf16x8s q[TILES][kTerms][kSteps];
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) {
+        const int row = row0 + u * kTile + n16;
+        const bool live = row < row_end;
+        const int at = live ? row / a.group : 0;
+        limit[u] = live ? seen_by(a, len, count, at) : a.max_tokens;
+        const T* src = static_cast<const T*>(a.q) + b * a.qs[0] +
+                       (g * a.group + (live ? row - at * a.group : 0)) * a.qs[1] + at * a.qs[2];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            Packet<T> p{};
+            if (live) load_packet(p, src + (s >> 1) * 64 + g4 * 16 + (s & 1) * 8);
+            float f[8];
+            unpack(p, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __bf16 w[kTerms];
+                split_bf16<kTerms>(f[i], w);
+#pragma unroll
+                for (int m = 0; m < kTerms; ++m) q[u][m][s][i] = w[m];
+            }
+        }
+    }
+    f32x4 o[TILES][kDims];
+    float top[TILES], base[TILES], sum[TILES];
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) {
+#pragma unroll
+        for (int j = 0; j < kDims; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        top[u] = -kInf;
+        base[u] = 0.0f;
+        sum[u] = 0.0f;
+    }
+
+    // Lane l looks up this wave's tile of the l-th of 64 steps.
+    const int64_t head = static_cast<int64_t>(g) * (D << a.page_shift);
+    const int page_mask = (1 << a.page_shift) - 1;
+    int page = -1;
+    float ks = 1.0f, vs = 1.0f;
+    auto look_up = [&](int seg) {
+        const int mine = seg + lane * kRowStep + wave * kTile;
+        page = -1;
+        if (mine < k1) page = a.pages[b * a.pages_stride + (mine >> a.page_shift)];
+        if (page >= a.num_pages || page < 0) page = -1;
+        ks = vs = 1.0f;
+        if (page >= 0) {
+            const int64_t at = static_cast<int64_t>(page) * a.G + g;
+            ks = a.k_scale[at];
+            vs = a.v_scale[at];
+        }
+    };
+    // A step's bytes of this wave's tile, loaded a step ahead.
+    struct Raw {
+        u32x4 k[kHalves];                // 1 KB each of the tile's rows in order
+        uint32_t v[4][kHalves];          // keys 4 g4 + r, dimensions n16 * kDims ..
+        int page;
+        float ks, vs;
+    };
+    auto fetch = [&](int step, Raw& x) {
+        const int i = step & 63;         // within the segment looked up
+        x.page = __builtin_amdgcn_readlane(page, i);
+        x.ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), i));
+        x.vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), i));
+        const int64_t pg = max(x.page, 0);
+        const int64_t row = head + ((k0 + step * kRowStep + wave * kTile) & page_mask) * D;
+        const uint8_t* kp = a.k + pg * a.k_page + row;
+        const uint8_t* vp = a.v + pg * a.v_page + row;
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+            x.k[h] = *reinterpret_cast<const u32x4*>(kp + lane * 16 + h * 1024);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint8_t* p = vp + (4 * g4 + r) * D + n16 * kDims;
+            if constexpr (kHalves == 2) {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+                x.v[r][0] = w.x;
+                x.v[r][kHalves - 1] = w.y;
+            } else {
+                x.v[r][0] = *reinterpret_cast<const uint32_t*>(p);
+            }
+        }
+    };
+    const int steps = k1 > k0 ? (k1 - k0 + kRowStep - 1) / kRowStep : 0;
+    // The step behind the last, and tiles without a page, load from page 0, unused.
+    Raw x;
+    look_up(k0);
+    fetch(0, x);
+#pragma unroll 1
+    for (int st = 0; st < steps; ++st) {
+        const int key = k0 + st * kRowStep;
+        __syncthreads();                         // all have read the step before
+        // widen this wave's tile
+        {
+            const int pg = x.page;
+            const float ksc = x.ks, vsc = x.vs;
+            bool bad = false;
+            if (key + kRowStep > least || pg < 0) {
+                // what no row sees may hold anything; a NaN that some row sees is set apart
+                const int there = pg < 0 ? key : most;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool in = key + wave * kTile + 4 * g4 + r < there;
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h) {
+                        uint32_t w = in ? x.v[r][h] : 0u;
+                        const uint32_t n = nan_bytes(w) >> 7;
+                        bits |= ((n & 1u) | (n >> 7 & 2u) | (n >> 14 & 4u) | (n >> 21 & 8u))
+                                << (4 * h);
+                        x.v[r][h] = w & ~(n * 0xFFu);
+                    }
+                    lds.nan[wave][4 * g4 + r][n16] = static_cast<uint8_t>(bits);
+                    bad = bad || bits != 0;
+                }
+            }
+            const uint64_t any = __ballot(bad);
+            if (lane == 0) lds.state[wave] = (pg < 0 ? kNoPage : 0) | (any != 0 ? kLost : 0);
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                // lane's 16 bytes: row r, chunk c = 4 e' + g' holds operands 2 e', 2 e' + 1
+                const int r = (h * 64 + lane) / kChunks, c = lane % kChunks;
+                const int slot = (c & 3) * kTile + (r ^ c);
+                lds.k[wave][2 * (c >> 2)][slot] = widen8(x.k[h].x, x.k[h].y, ksc);
+                lds.k[wave][2 * (c >> 2) + 1][slot] = widen8(x.k[h].z, x.k[h].w, ksc);
+            }
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                uint32_t lo[2], hi[2];
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    lo[p] = __builtin_amdgcn_perm(x.v[2 * p + 1][h], x.v[2 * p][h], 0x05010400u);
+                    hi[p] = __builtin_amdgcn_perm(x.v[2 * p + 1][h], x.v[2 * p][h], 0x07030602u);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    u32x2 w = {pack_bf16(j < 2 ? lo[0] : hi[0], vsc, j & 1),
+                               pack_bf16(j < 2 ? lo[1] : hi[1], vsc, j & 1)};
+                    lds.v[wave >> 1][4 * h + j][lane][wave & 1] = w;
+                }
+            }
+        }
+        if (((st + 1) & 63) == 0) look_up(key + kRowStep);
+        fetch(st + 1, x);
+        __syncthreads();
+        if (row0 >= row_end) continue;
+        int any = 0, there[4];                   // first key of a tile that no page holds
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int state = __builtin_amdgcn_readfirstlane(lds.state[t]);
+            there[t] = state & kNoPage ? key : most;
+            any |= state;
+        }
+        const bool whole = key + kRowStep <= least && any == 0;
+        const bool lost = (any & kLost) != 0;
+        // Operands are read from LDS a group ahead of the products that take them; the
+        // scheduling fences keep the compiler from sinking the reads to their use, where each
+        // would be waited for alone.
+        auto key_operands = [&](int t, bf16x8s (&kf)[kSteps]) {
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e)
+                kf[e] = lds.k[t][e][g4 * kTile + (n16 ^ (4 * (e >> 1) + g4))];
+        };
+        constexpr int kGroup = 4;
+        auto value_operands = [&](int i, bf16x8s (&vf)[kGroup]) {
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j)
+                vf[j] = *reinterpret_cast<const bf16x8s*>(
+                    &lds.v[i / kHalves][kGroup * (i % kHalves) + j][lane][0]);
+        };
+        f32x4 s[TILES][4];
+        bf16x8s kf[2][kSteps], vf[2][kGroup];
+        key_operands(0, kf[0]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (t < 3) key_operands(t + 1, kf[(t + 1) & 1]);
+            else value_operands(0, vf[0]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < TILES; ++u) s[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e)
+#pragma unroll
+                for (int u = 0; u < TILES; ++u)
+#pragma unroll
+                    for (int m = kTerms - 1; m >= 0; --m)
+                        s[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t & 1][e], q[u][m][e],
+                                                                          s[u][t], 0, 0, 0);
+        }
+        bf16x8s pf[TILES][2][kParts];
+#pragma unroll
+        for (int u = 0; u < TILES; ++u) {
+            float y[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = s[u][i >> 2][i & 3];
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int kk = key + (i >> 2) * kTile + 4 * g4 + (i & 3);
+                    if (kk >= min(limit[u], there[i >> 2])) y[i] = -kInf;
+                }
+            }
+            if (a.logits) {
+                const int row = row0 + u * kTile + n16;
+                if (row < row_end) {
+                    float* to = a.logits +
+                                ((b * a.G + g) * static_cast<int64_t>(a.rows) + row) *
+                                    a.logit_stride + key + 4 * g4;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        *reinterpret_cast<f32x4*>(to + t * kTile) =
+                            f32x4{y[4 * t] * a.scale, y[4 * t + 1] * a.scale,
+                                  y[4 * t + 2] * a.scale, y[4 * t + 3] * a.scale};
+                }
+            }
+            weigh<16, kDims>(y, a.scale, top[u], base[u], sum[u], o[u]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                __bf16 w[kParts];
+                split_bf16<kParts>(y[i], w);
+#pragma unroll
+                for (int m = 0; m < kParts; ++m) pf[u][i >> 3][m][i & 7] = w[m];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * kHalves; ++i) {
+            if (i + 1 < 2 * kHalves) value_operands(i + 1, vf[(i + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            const int h = i / kHalves, j0 = kGroup * (i % kHalves);
+#pragma unroll
+            for (int m = kParts - 1; m >= 0; --m)
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j)
+#pragma unroll
+                    for (int u = 0; u < TILES; ++u)
+                        o[u][j0 + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            vf[i & 1][j], pf[u][h][m], o[u][j0 + j], 0, 0, 0);
+        }
+        if (lost) {
+            // a NaN value reaches the rows that see its key, and no other
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < kDims; ++j) {
+                    bf16x8s nans;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        nans[i] = static_cast<__bf16>(
+                            (lds.nan[2 * h + (i >> 2)][4 * g4 + (i & 3)][n16] >> j) & 1
+                                ? 1.0f : 0.0f);
+#pragma unroll
+                    for (int u = 0; u < TILES; ++u) {
+                        bf16x8s seen;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int kk = key + (2 * h + (i >> 2)) * kTile + 4 * g4 + (i & 3);
+                            seen[i] = static_cast<__bf16>(kk < limit[u] ? 1.0f : 0.0f);
+                        }
+                        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                        const f32x4 hits =
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(nans, seen, zero, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (hits[r] > 0.0f) o[u][j][r] = __builtin_nanf("");
+                    }
+                }
+            }
+        }
+    }
+
+    // each wave has its rows' whole sums: lane (n, g4) holds dimensions (4 g4 + r) kDims + j
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) {
+        const int row = row0 + u * kTile + n16;
+        float total = sum[u];
+        total += __shfl_xor(total, 16);
+        total += __shfl_xor(total, 32);
+        if (row >= row_end) continue;
+        const int64_t line = (b * a.G + g) * static_cast<int64_t>(a.rows) + row;
+        if (a.splits == 1) {
+            const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+            const int t = row / a.group;
+            T* to = static_cast<T*>(a.out) + b * a.os[0] +
+                    (g * a.group + row - t * a.group) * a.os[1] + t * a.os[2] + 4 * g4 * kDims;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                Run<T, kDims> z;
+#pragma unroll
+                for (int j = 0; j < kDims; ++j) z.x[j] = from_f32<T>(o[u][j][r] * inv);
+                *reinterpret_cast<Run<T, kDims>*>(to + r * kDims) = z;
+            }
+            if (a.lse && g4 == 0)
+                a.lse[line] = total > 0.0f || total != total ? top[u] + __log2f(total) : -kInf;
+        } else {
+            const int64_t part = line * a.splits + split;
+            float* to = a.part_out + part * D + 4 * g4 * kDims;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                Run<float, kDims> z;
+#pragma unroll
+                for (int j = 0; j < kDims; ++j) z.x[j] = o[u][j][r];
+                *reinterpret_cast<Run<float, kDims>*>(to + r * kDims) = z;
+            }
+            if (g4 == 0) {
+                a.part_max[part] = top[u];
+                a.part_sum[part] = total;
+            }
+        }
+    }
+}
+
+// Joins the parts of a row, WAVES waves to a row (several where the parts are many, and
+// reading them one after the other would take long); `line` counts rows over all (sequence,
+// key head).  A part is there where its first key is seen by the workgroup that wrote it;
+// parts whose keys this row does not see hold a maximum of -inf.
+template <typename T, int D, int WAVES>
+__device__ __forceinline__ void join_rows(const AttendArgs& a, int64_t block, int64_t lines) {
+    constexpr int kRows = kAttendWaves / WAVES;
+    __shared__ float merge[kRows][WAVES][D];
+    __shared__ float sums[kRows][WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int which = wave / WAVES, sub = wave % WAVES;
+    const int64_t line = block * kRows + which;
+    const int64_t bg = line < lines ? line / a.rows : 0;
     const int row = static_cast<int>(line - bg * a.rows);
     const int64_t b = bg / a.G;
     const int g = static_cast<int>(bg - b * a.G);
     const int len = attend_length(a, b), count = attend_count(a, b);
     const int t = row / a.group;
-    if (t >= count) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int limit = seen_by(a, len, count, t);
+    const bool live = line < lines && t < count;
+    const int limit = live ? seen_by(a, len, count, t) : 0;
     const int parts = static_cast<int>((limit + a.chunk - 1) / a.chunk);   // <= splits
     constexpr int kPer = D / 64;
     float m = -kInf;
     for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.part_max[line * a.splits + i]);
     m = wave_max(m);
     float total = 0.0f, y[kPer] = {};
-#pragma unroll 4
-    for (int i = wave; i < parts; i += kAttendWaves) {
+#pragma unroll 8
+    for (int i = sub; i < parts; i += WAVES) {
         const int64_t part = line * a.splits + i;
         const float pm = a.part_max[part];      // -inf: the part holds zeros, or NaN
         const float f = pm == -kInf ? 1.0f : exp2_hw(pm - m);
@@ -608,72 +1038,135 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(const AttendArgs 
 #pragma unroll
         for (int k = 0; k < kPer; ++k) y[k] += a.part_out[part * D + lane * kPer + k] * f;
     }
+    if constexpr (WAVES > 1) {
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) merge[wave][lane * kPer + k] = y[k];
-    if (lane == 0) sums[wave] = total;
-    __syncthreads();
-    total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-    if (threadIdx.x < D) {
-        const int d = threadIdx.x;
-        const float z = (merge[0][d] + merge[1][d]) + (merge[2][d] + merge[3][d]);
-        T* to = static_cast<T*>(a.out) + b * a.os[0] +
-                (g * a.group + row - t * a.group) * a.os[1] + t * a.os[2];
-        to[d] = from_f32<T>(z * inv);
+        for (int k = 0; k < kPer; ++k) merge[which][sub][lane * kPer + k] = y[k];
+        if (lane == 0) sums[which][sub] = total;
+        __syncthreads();
+        total = sums[which][0];
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) y[k] = merge[which][0][lane * kPer + k];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            total += sums[which][w];
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) y[k] += merge[which][w][lane * kPer + k];
+        }
     }
-    if (a.lse && threadIdx.x == 0)
-        a.lse[line] = total > 0.0f || total != total ? m + __log2f(total)
-                                                     : -kInf;
+    if (!live || sub != 0) return;
+    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+    T* to = static_cast<T*>(a.out) + b * a.os[0] + (g * a.group + row - t * a.group) * a.os[1] +
+            t * a.os[2] + lane * kPer;
+    Run<T, kPer> z;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) z.x[k] = from_f32<T>(y[k] * inv);
+    *reinterpret_cast<Run<T, kPer>*>(to) = z;
+    if (a.lse && lane == 0)
+        a.lse[line] = total > 0.0f || total != total ? m + __log2f(total) : -kInf;
 }
 
-// The weight that every token received: sum over the rows of exp2(logit - lse), from the
-// stored logits, rows in order.  One thread takes four neighbouring tokens.
-__global__ __launch_bounds__(kThreads) void attend_weights_kernel(const AttendArgs a, int blocks) {
-    const int64_t bg = blockIdx.x / blocks;
+// log2 of the sums of up to kFewRows rows, from their parts, into LDS: a wave to a row.
+constexpr int kFewRows = 32;
+__device__ __forceinline__ void sums_of_parts(const AttendArgs& a, int64_t bg, int len, int count,
+                                              float* lse) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int row = wave; row < count * a.group; row += kAttendWaves) {
+        const int limit = seen_by(a, len, count, row / a.group);
+        const int parts = static_cast<int>((limit + a.chunk - 1) / a.chunk);
+        const int64_t first = (bg * a.rows + row) * a.splits;
+        float m = -kInf;
+        for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.part_max[first + i]);
+        m = wave_max(m);
+        float total = 0.0f;
+        for (int i = lane; i < parts; i += 64) {
+            const float pm = a.part_max[first + i];
+            total += a.part_sum[first + i] * (pm == -kInf ? 1.0f : exp2_hw(pm - m));
+        }
+        total = wave_sum(total);
+        if (lane == 0) lse[row] = total > 0.0f || total != total ? m + __log2f(total) : -kInf;
+    }
+    __syncthreads();
+}
+
+// What is left after the parts: the rows' joins (the first `joins` workgroups) and, where
+// weights are wanted and the rows are few, the tokens' weights (`blocks` workgroups to a
+// (sequence, key head), four neighbouring tokens to a thread).
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(kThreads) void attend_finish_kernel(const AttendArgs a, int64_t lines,
+                                                                 uint32_t joins, uint32_t blocks) {
+    if (blockIdx.x < joins) {
+        join_rows<T, D, WAVES>(a, blockIdx.x, lines);
+        return;
+    }
+    __shared__ float lse[kFewRows];
+    const uint32_t id = blockIdx.x - joins;
+    const int64_t bg = id / blocks;
     const int64_t b = bg / a.G;
-    const int g = static_cast<int>(bg - b * a.G);
-    const int n0 = (static_cast<int>(blockIdx.x - bg * blocks) * kThreads +
-                    static_cast<int>(threadIdx.x)) * 4;
+    const int n0 = static_cast<int>(id % blocks) * 4 * kThreads;
     const int len = attend_length(a, b), count = attend_count(a, b);
     if (n0 >= len) return;
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
-    const int rows = count * a.group;
-    for (int row = 0; row < rows; ++row) {
-        const int limit = seen_by(a, len, count, row / a.group);
-        if (n0 >= limit) continue;
-        const int64_t line = bg * a.rows + row;
-        const float l = a.lse[line];
-        if (l == -kInf) continue;
-        const f32x4 x = *reinterpret_cast<const f32x4*>(a.logits + line * a.logit_stride + n0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] += n0 + i < limit ? exp2_hw(x[i] - l) : 0.0f;
-    }
-    const float* in = a.w_in ? a.w_in + b * a.wi[0] + g * a.wi[1] : nullptr;
-    float* out = a.w_out + b * a.wo[0] + g * a.wo[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (n0 + i < len) out[n0 + i] = in ? in[n0 + i] + w[i] : w[i];
+    sums_of_parts(a, bg, len, count, lse);
+    token_weights(a, b, static_cast<int>(bg - b * a.G), lse, len, count,
+                  n0 + static_cast<int>(threadIdx.x) * 4, a.max_tokens);
+}
+
+// The tokens' weights from rows whose sums lie in the workspace.
+__global__ __launch_bounds__(kThreads) void attend_weights_kernel(const AttendArgs a,
+                                                                  uint32_t blocks) {
+    const int64_t bg = blockIdx.x / blocks;
+    const int64_t b = bg / a.G;
+    const int n0 = (static_cast<int>(blockIdx.x % blocks) * kThreads +
+                    static_cast<int>(threadIdx.x)) * 4;
+    token_weights(a, b, static_cast<int>(bg - b * a.G), a.lse + bg * a.rows,
+                  attend_length(a, b), attend_count(a, b), n0, a.max_tokens);
 }
 
 template <typename T, int D>
 hipError_t launch_t(const AttendArgs& a, const AttendPlan& p, int64_t B, hipStream_t st) {
-    const dim3 grid(static_cast<unsigned>(B * a.G * a.splits * a.row_groups));
-    if (p.tiles == 1)
-        hipLaunchKernelGGL((attend_kernel<T, D, 1>), grid, dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL((attend_kernel<T, D, 2>), grid, dim3(kThreads), 0, st, a);
+    const dim3 grid(static_cast<unsigned>(B * a.G * a.splits * a.row_groups)), block(kThreads);
+    if (p.shared_rows) {
+        if constexpr (Terms<T>::n == 1) {
+            if (p.tiles == 2)
+                hipLaunchKernelGGL((attend_rows_kernel<T, D, 2>), grid, block, 0, st, a);
+        }
+        if (p.tiles == 1)
+            hipLaunchKernelGGL((attend_rows_kernel<T, D, 1>), grid, block, 0, st, a);
+    } else if (p.waves == 8) {
+        if (p.tiles == 1)
+            hipLaunchKernelGGL((attend_kernel<T, D, 1, 8>), grid, dim3(512), 0, st, a);
+        else
+            hipLaunchKernelGGL((attend_kernel<T, D, 2, 8>), grid, dim3(512), 0, st, a);
+    } else {
+        if (p.tiles == 1)
+            hipLaunchKernelGGL((attend_kernel<T, D, 1, 4>), grid, block, 0, st, a);
+        else
+            hipLaunchKernelGGL((attend_kernel<T, D, 2, 4>), grid, block, 0, st, a);
+    }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
+    const int64_t lines = B * a.G * a.rows;
+    const uint32_t blocks = static_cast<uint32_t>((a.max_tokens + 4 * kThreads - 1) /
+                                                  (4 * kThreads));
     if (a.splits > 1) {
-        hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3(static_cast<unsigned>(B * a.G * a.rows)),
-                           dim3(kThreads), 0, st, a);
+        // the weights of few rows in the same launch
+        const uint32_t more =
+            a.w_out && !p.lse_kept ? static_cast<uint32_t>(B * a.G) * blocks : 0u;
+        if (a.splits > 8) {
+            const uint32_t joins = static_cast<uint32_t>(lines);
+            hipLaunchKernelGGL((attend_finish_kernel<T, D, kAttendWaves>), dim3(joins + more),
+                               block, 0, st, a, lines, joins, blocks);
+        } else {
+            const uint32_t joins =
+                static_cast<uint32_t>((lines + kAttendWaves - 1) / kAttendWaves);
+            hipLaunchKernelGGL((attend_finish_kernel<T, D, 1>), dim3(joins + more), block, 0, st,
+                               a, lines, joins, blocks);
+        }
         err = hipGetLastError();
         if (err != hipSuccess) return err;
     }
-    if (a.w_out) {
-        const int blocks = (a.max_tokens + 4 * kThreads - 1) / (4 * kThreads);
-        hipLaunchKernelGGL(attend_weights_kernel, dim3(static_cast<unsigned>(B * a.G * blocks)),
-                           dim3(kThreads), 0, st, a, blocks);
+    if (a.w_out && p.lse_kept) {
+        hipLaunchKernelGGL(attend_weights_kernel,
+                           dim3(static_cast<unsigned>(B * a.G) * blocks), block, 0, st, a, blocks);
         err = hipGetLastError();
     }
     return err;
@@ -714,7 +1207,7 @@ hipError_t launch_cache_attend(const e2s_cache& c, const e2s_cache_attend_shape&
         a.part_out = reinterpret_cast<float*>(ws + p.part_off);
     }
     if (weights_out) {
-        a.lse = reinterpret_cast<float*>(ws + p.lse_off);
+        if (p.lse_kept) a.lse = reinterpret_cast<float*>(ws + p.lse_off);
         a.logits = reinterpret_cast<float*>(ws + p.logit_off);
     }
     a.logit_stride = p.logit_stride;

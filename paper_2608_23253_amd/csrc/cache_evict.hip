@@ -6,12 +6,14 @@
 // digit by digit (11, 11 and 10 bits) from a histogram in LDS.  Tokens above it stay, and
 // of those equal to it the first ones; counts per wave and a scan over the waves place the
 // kept tokens in ascending order.  All decisions are on integers, so nothing depends on
-// the order of the atomic increments.  Each pass reads the weights again: 4 bytes per
-// token, from L2 after the first.
+// the order of the atomic increments.  Latency bounds it: a thread loads its keys (up to 16)
+// at once and keeps them in registers for all passes where the sequences fit one segment of
+// 1024 x 16 tokens; longer ones are read again, a segment at a time, in every pass.
 //
-// evict_move_kernel, one workgroup per (sequence, key head, new block, keys or values):
-// gathers the block's kept rows, takes their largest magnitude to the block's scale, and
-// writes them rescaled by the ratio of two powers of two.  It moves each kept byte once.
+// evict_move_kernel, one workgroup per (sequence, key head, new block), keys and values
+// together (they share the lookups of indices and pages): gathers the block's kept rows,
+// takes their largest magnitude to the block's scale, and writes them rescaled by the ratio
+// of two powers of two.  It moves each kept byte once, and the copy rate bounds it.
 #include "serve_device.h"
 #include "serve_kernels.h"
 
@@ -36,7 +38,7 @@ struct EvictArgs {
     int64_t page_stride[2];
     int64_t pages_stride, new_pages_stride;
     int64_t ws[2], ls[2];
-    int G, P, K, W, sinks, recent, max_tokens, max_pages, num_pages, blocks;
+    int G, P, page_shift, K, W, sinks, recent, max_tokens, max_pages, num_pages, blocks;
 };
 
 __device__ __forceinline__ int evict_length(const EvictArgs& a, int64_t b) {
@@ -50,12 +52,15 @@ __device__ __forceinline__ uint32_t rank_key(float w) {
     return w != w ? 0u : ordered_bits(w + 0.0f);
 }
 
+template <int PER>                       // tokens per thread and segment
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
     __shared__ uint32_t hist[kBins];
     __shared__ uint32_t sums[kSelWaves];
     __shared__ uint32_t ties[kSelWaves];
     __shared__ uint32_t found[2];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    constexpr int kSegment = kSelThreads * PER;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int64_t b = blockIdx.x / a.G;
     const int g = static_cast<int>(blockIdx.x - b * a.G);
     const int n = evict_length(a, b);
@@ -76,6 +81,18 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
     }
     // sinks + recent <= K < n: the ends do not meet, and m0 < m1
     const int m0 = a.sinks, m1 = n - a.recent;
+    // A wave holds PER runs of 64 neighbouring tokens of a segment, one after the other.
+    float x[PER];
+    auto token = [&](int seg, int j) { return seg + (wave * PER + j) * kWave + lane; };
+    auto load = [&](int seg) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int i = token(seg, j);
+            x[j] = i < n ? w[i] : 0.0f;
+        }
+    };
+    const bool once = n <= kSegment;
+    if (once) load(0);
     uint32_t want = static_cast<uint32_t>(a.K - a.sinks - a.recent);
     // keys above `limit` stay, and of the keys equal to it the first `want`
     uint32_t limit = 0xFFFFFFFFu;
@@ -86,11 +103,18 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
             const uint32_t mask = pass == 2 ? 1023u : 2047u;
-            for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+            hist[tid] = 0;
+            hist[tid + kSelThreads] = 0;
             __syncthreads();
-            for (int i = m0 + tid; i < m1; i += kSelThreads) {
-                const uint32_t key = rank_key(w[i]);
-                if ((key & known) == limit) atomicAdd(&hist[(key >> shift) & mask], 1u);
+            for (int seg = 0; seg < n; seg += kSegment) {
+                if (!once) load(seg);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int i = token(seg, j);
+                    const uint32_t key = rank_key(x[j]);
+                    if (i >= m0 && i < m1 && (key & known) == limit)
+                        atomicAdd(&hist[(key >> shift) & mask], 1u);
+                }
             }
             __syncthreads();
             // thread t owns bins 2047 - 2t and 2046 - 2t: sums from the top
@@ -103,7 +127,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
             if (lane == kWave - 1) sums[wave] = run;
             __syncthreads();
             uint32_t above = run - (h1 + h0);
-            for (int v = 0; v < wave; ++v) above += sums[v];
+#pragma unroll
+            for (int v = 0; v < kSelWaves; ++v) above += v < wave ? sums[v] : 0u;
             // the digit at which the count from the top reaches `want`
             if (above < want && above + h1 + h0 >= want) {
                 const bool upper = above + h1 >= want;
@@ -114,134 +139,156 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
             limit |= found[0] << shift;
             want = found[1];
             known |= mask << shift;
-            __syncthreads();
         }
     }
-    // every wave takes a run of tokens, whole groups of 64
-    const int per = (n + kSelThreads - 1) / kSelThreads * kWave;
-    const int i0 = wave * per, i1 = min(n, i0 + per);
-    uint32_t more = 0, same = 0;
-    for (int i = i0 + lane; i - lane < i1; i += kWave) {
-        bool up = false, tie = false;
-        if (i < i1) {
-            up = i < m0 || i >= m1;
-            if (!up) {
-                const uint32_t key = rank_key(w[i]);
-                up = key > limit;
-                tie = key == limit;
+    // Per segment: every wave counts its tokens that stay and its ties, then places them.
+    uint32_t more = 0, same = 0;                       // of the segments before
+    for (int seg = 0; seg < n; seg += kSegment) {
+        if (!once) load(seg);
+        uint64_t ups[PER], equal[PER];
+        uint32_t up_here = 0, tie_here = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int i = token(seg, j);
+            const uint32_t key = rank_key(x[j]);
+            const bool end = i < m0 || i >= m1;
+            ups[j] = __ballot(i < n && (end || key > limit));
+            equal[j] = __ballot(i < n && !end && key == limit);
+            up_here += __popcll(ups[j]);
+            tie_here += __popcll(equal[j]);
+        }
+        __syncthreads();                               // sums and ties are free
+        if (lane == 0) {
+            sums[wave] = up_here;
+            ties[wave] = tie_here;
+        }
+        __syncthreads();
+        uint32_t before = same, slot0 = more;
+#pragma unroll
+        for (int v = 0; v < kSelWaves; ++v) {
+            slot0 += v < wave ? sums[v] : 0u;
+            before += v < wave ? ties[v] : 0u;
+            more += sums[v];
+            same += ties[v];
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const uint64_t below = (uint64_t{1} << lane) - 1;
+            const uint32_t tie = before + __popcll(equal[j] & below);
+            const bool stays = (ups[j] >> lane & 1) || ((equal[j] >> lane & 1) && tie < want);
+            if (stays) {                               // K tokens in all, so slot < K
+                const uint32_t slot = slot0 + __popcll(ups[j] & below) + min(tie, want);
+                keep[slot] = token(seg, j);
+                if (left) left[slot] = x[j];
             }
+            slot0 += __popcll(ups[j]);
+            before += __popcll(equal[j]);
         }
-        more += __popcll(__ballot(up));
-        same += __popcll(__ballot(tie));
-    }
-    if (lane == 0) {
-        sums[wave] = more;
-        ties[wave] = same;
-    }
-    __syncthreads();
-    more = same = 0;
-    for (int v = 0; v < wave; ++v) {
-        more += sums[v];
-        same += ties[v];
-    }
-    for (int i = i0 + lane; i - lane < i1; i += kWave) {
-        bool up = false, tie = false;
-        float x = 0.0f;
-        if (i < i1) {
-            x = w[i];
-            up = i < m0 || i >= m1;
-            if (!up) {
-                const uint32_t key = rank_key(x);
-                up = key > limit;
-                tie = key == limit;
-            }
-        }
-        const uint64_t ups = __ballot(up), equal = __ballot(tie);
-        const uint64_t below = (uint64_t{1} << lane) - 1;
-        const uint32_t before = same + __popcll(equal & below);
-        if (up || (tie && before < want)) {       // K tokens in all, so slot < K
-            const uint32_t slot = more + __popcll(ups & below) + min(before, want);
-            keep[slot] = i;
-            if (left) left[slot] = x;
-        }
-        more += __popcll(ups);
-        same += __popcll(equal);
     }
 }
 
-// PACKETS packets of 16 bytes per thread cover a block.
+// PACKETS packets of 16 bytes per thread cover a block of keys, and as many its values.
 template <int D, int THREADS, int PACKETS>
 __global__ __launch_bounds__(THREADS) void evict_move_kernel(const EvictArgs a) {
     constexpr int kLanes = D / 16;
-    __shared__ float shared[THREADS / kWave];
-    const int which = blockIdx.x & 1;
-    const int64_t unit = blockIdx.x >> 1;
-    const int g = static_cast<int>(unit % a.G);
-    const int64_t ub = unit / a.G;
-    const int64_t b = ub / a.blocks;
-    const int blk = static_cast<int>(ub - b * a.blocks);
+    __shared__ float shared[2][THREADS / kWave];
+    const uint32_t unit = blockIdx.x;
+    const int g = static_cast<int>(unit % static_cast<uint32_t>(a.G));
+    const uint32_t ub = unit / static_cast<uint32_t>(a.G);
+    const int64_t b = ub / static_cast<uint32_t>(a.blocks);
+    const int blk = static_cast<int>(ub % static_cast<uint32_t>(a.blocks));
     const int kept = min(evict_length(a, b), a.K);
-    const int first = blk * a.P;
+    const int first = blk << a.page_shift;
     if (first >= kept) return;
     const int page = a.new_pages[b * a.new_pages_stride + blk];
     if (page < 0 || page >= a.num_pages) return;
     const int rows = min(kept - first, a.P);
     const int32_t* keep = a.keep + (b * a.G + g) * static_cast<int64_t>(a.K) + first;
-    const int64_t head = static_cast<int64_t>(g) * a.P * D;
+    const int64_t head = static_cast<int64_t>(g) * (D << a.page_shift);
 
-    u32x4 x[PACKETS];
-    float from[PACKETS];
-    float top = 0.0f;
+    u32x4 x[PACKETS][2];
+    float from[PACKETS][2];
+    int idx[PACKETS], src[PACKETS];
 #pragma unroll
     for (int p = 0; p < PACKETS; ++p) {
-        const int i = p * THREADS + threadIdx.x;
-        const int r = i / kLanes, c = i - r * kLanes;
-        x[p] = u32x4{0u, 0u, 0u, 0u};
-        from[p] = 1.0f;
-        if (r >= rows) continue;
-        const int idx = keep[r];                    // 0 <= idx < length <= max_pages * P
-        const int src = a.pages[b * a.pages_stride + idx / a.P];
-        if (src < 0 || src >= a.num_pages) continue;
-        from[p] = a.scale[which][static_cast<int64_t>(src) * a.G + g];
-        x[p] = *reinterpret_cast<const u32x4*>(a.src[which] + src * a.page_stride[which] + head +
-                                               static_cast<int64_t>(idx % a.P) * D + c * 16);
+        const int r = (p * THREADS + static_cast<int>(threadIdx.x)) / kLanes;
+        idx[p] = r < rows ? keep[r] : -1;           // < length <= max_pages * P
     }
 #pragma unroll
     for (int p = 0; p < PACKETS; ++p) {
-        const uint32_t word[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+        src[p] = idx[p] >= 0 ? a.pages[b * a.pages_stride + (idx[p] >> a.page_shift)] : -1;
+        if (src[p] >= a.num_pages) src[p] = -1;
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float v[4];
-            from_e4m3(word[i], v);
+    for (int p = 0; p < PACKETS; ++p)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)             // a NaN is no maximum
-                top = fmaxf(top, v[k] == v[k] ? fabsf(v[k]) * from[p] : 0.0f);
+        for (int k = 0; k < 2; ++k) {
+            x[p][k] = u32x4{0u, 0u, 0u, 0u};
+            from[p][k] = 1.0f;
+            if (src[p] < 0) continue;
+            from[p][k] = a.scale[k][static_cast<int64_t>(src[p]) * a.G + g];
+            const int row = idx[p] & (a.P - 1);
+            const int c = static_cast<int>(threadIdx.x) % kLanes;
+            x[p][k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+                a.src[k] + src[p] * a.page_stride[k] + head + row * D + c * 16));
+        }
+    float to[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        float top = 0.0f;
+#pragma unroll
+        for (int p = 0; p < PACKETS; ++p) {
+            const uint32_t word[4] = {x[p][k].x, x[p][k].y, x[p][k].z, x[p][k].w};
+            float most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[4];
+                from_e4m3(word[i], v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(v[e]));   // skips NaN
+            }
+            top = fmaxf(top, most * from[p][k]);
+        }
+        top = wave_max(top);
+        if ((threadIdx.x & (kWave - 1)) == 0) shared[k][threadIdx.x / kWave] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        float top = shared[k][0];
+#pragma unroll
+        for (int v = 1; v < THREADS / kWave; ++v) top = fmaxf(top, shared[k][v]);
+        to[k] = block_scale(top);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        uint8_t* out = a.dst[k] + page * a.page_stride[k] + head;
+#pragma unroll
+        for (int p = 0; p < PACKETS; ++p) {
+            const int i = p * THREADS + static_cast<int>(threadIdx.x);
+            if (i / kLanes >= rows) continue;
+            u32x4 w = x[p][k];
+            if (from[p][k] != to[k]) {
+                const float ratio = scale_ratio(from[p][k], to[k]);
+                w.x = rescale_e4m3(w.x, ratio);
+                w.y = rescale_e4m3(w.y, ratio);
+                w.z = rescale_e4m3(w.z, ratio);
+                w.w = rescale_e4m3(w.w, ratio);
+            }
+            *(reinterpret_cast<u32x4*>(out) + i) = w;
         }
     }
-    top = block_max<THREADS>(top, shared);
-    const float to = block_scale(top);
-    uint8_t* out = a.dst[which] + page * a.page_stride[which] + head;
-#pragma unroll
-    for (int p = 0; p < PACKETS; ++p) {
-        const int i = p * THREADS + threadIdx.x;
-        if (i / kLanes >= rows) continue;
-        u32x4 w = x[p];
-        if (from[p] != to) {
-            const float ratio = scale_ratio(from[p], to);
-            w.x = rescale_e4m3(w.x, ratio);
-            w.y = rescale_e4m3(w.y, ratio);
-            w.z = rescale_e4m3(w.z, ratio);
-            w.w = rescale_e4m3(w.w, ratio);
-        }
-        *(reinterpret_cast<u32x4*>(out) + i) = w;
+    if (threadIdx.x == 0) {
+        const int64_t at = static_cast<int64_t>(page) * a.G + g;
+        a.scale[0][at] = to[0];
+        a.scale[1][at] = to[1];
     }
-    if (threadIdx.x == 0) a.scale[which][static_cast<int64_t>(page) * a.G + g] = to;
 }
 
 template <int D, int THREADS, int PACKETS>
 void launch_move_k(const EvictArgs& a, int64_t B, hipStream_t st) {
     hipLaunchKernelGGL((evict_move_kernel<D, THREADS, PACKETS>),
-                       dim3(static_cast<unsigned>(2 * B * a.blocks * a.G)), dim3(THREADS), 0, st,
+                       dim3(static_cast<unsigned>(B * a.blocks * a.G)), dim3(THREADS), 0, st,
                        a);
 }
 
@@ -282,6 +329,7 @@ hipError_t launch_cache_evict(const e2s_cache& c, const e2s_cache_evict_shape& s
     }
     a.G = c.num_kv_heads;
     a.P = c.page_tokens;
+    a.page_shift = __builtin_ctz(static_cast<unsigned>(c.page_tokens));   // a power of two
     a.K = s.budget;
     a.W = s.left_tokens;
     a.sinks = s.sinks;
@@ -290,8 +338,13 @@ hipError_t launch_cache_evict(const e2s_cache& c, const e2s_cache_evict_shape& s
     a.max_pages = s.max_pages;
     a.num_pages = c.num_pages;
     a.blocks = (s.budget + c.page_tokens - 1) / c.page_tokens;
-    hipLaunchKernelGGL(evict_select_kernel, dim3(static_cast<unsigned>(s.batch * a.G)),
-                       dim3(kSelThreads), 0, st, a);
+    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(s.batch) * a.G));
+    if (s.max_tokens <= kSelThreads)
+        hipLaunchKernelGGL(evict_select_kernel<1>, grid, dim3(kSelThreads), 0, st, a);
+    else if (s.max_tokens <= 4 * kSelThreads)
+        hipLaunchKernelGGL(evict_select_kernel<4>, grid, dim3(kSelThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL(evict_select_kernel<16>, grid, dim3(kSelThreads), 0, st, a);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     if (c.head_dim == 64) launch_move<64>(a, s.batch, st);

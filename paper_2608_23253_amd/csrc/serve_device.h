@@ -68,18 +68,4 @@ __device__ __forceinline__ float scale_ratio(float from, float to) {
     return fminf(from / to, 1048576.0f);
 }
 
-// Largest of the values that the threads of a workgroup hold (all >= 0).
-template <int THREADS>
-__device__ __forceinline__ float block_max(float v, float* shared) {
-    v = wave_max(v);
-    if constexpr (THREADS > kWave) {
-        if ((threadIdx.x & (kWave - 1)) == 0) shared[threadIdx.x / kWave] = v;
-        __syncthreads();
-        v = shared[0];
-#pragma unroll
-        for (int w = 1; w < THREADS / kWave; ++w) v = fmaxf(v, shared[w]);
-    }
-    return v;
-}
-
 }  // namespace e2s

@@ -208,8 +208,7 @@ e2s_status check_attend(const e2s_cache& c, const e2s_cache_attend_shape* s) {
     const double heads = static_cast<double>(s->batch) * c.num_kv_heads;
     // every kernel of the call: fewer than 2^32 work-items
     if (heads * p.row_groups * p.splits * 256.0 >= 4294967296.0 ||
-        heads * p.rows * 256.0 >= 4294967296.0 ||
-        heads * ((s->max_tokens + 255) / 256) * 256.0 >= 4294967296.0)
+        heads * (static_cast<double>(p.rows) + (s->max_tokens + 255) / 256) * 256.0 >= 4294967296.0)
         return E2S_ERR_UNSUPPORTED;
     // and a workspace that 63 bits address
     if (heads * p.rows * (static_cast<double>(p.splits) * (c.head_dim + 2) + p.logit_stride) * 4.0 >
@@ -247,16 +246,30 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     AttendPlan p{};
     const int64_t B = s.batch, G = c.num_kv_heads, D = c.head_dim;
     p.rows = static_cast<int64_t>(s.num_heads) / G * s.num_queries;
-    p.tiles = p.rows <= 16 ? 1 : 2;
-    p.row_groups = (p.rows + 16 * p.tiles - 1) / (16 * p.tiles);
-    const int64_t unit = kAttendStep * kAttendWaves;
+    // Up to 32 rows, a workgroup's waves share the rows and part the keys; above, they part
+    // the rows (16 or 32 each) and share the keys' operands in LDS.
+    p.shared_rows = p.rows > 32;
+    const int64_t per_tile = p.shared_rows ? 16 * kAttendWaves : 16;
+    p.tiles = p.rows <= per_tile ? 1 : 2;
+    // 32 rows to a wave halve what is widened and read from LDS per row, where that still
+    // gives two workgroups to a compute unit; with queries in two or three parts they do not
+    // fit the registers.
+    if (p.shared_rows && (s.dtype != E2S_DTYPE_BF16 ||
+                          B * G * ((p.rows + 2 * per_tile - 1) / (2 * per_tile)) < 512))
+        p.tiles = 1;
+    p.row_groups = (p.rows + per_tile * p.tiles - 1) / (per_tile * p.tiles);
     const int64_t units = B * G * p.row_groups;
-    const int64_t want = 2048;      // workgroups that fill the device several times over
+    const int64_t want = p.shared_rows ? 1536 : 2048;   // workgroups that fill the device
     int64_t per = (s.max_tokens * units + want - 1) / want;
-    per = std::max<int64_t>(per, 2 * unit);
+    // Short sequences: one workgroup of eight waves has all keys, and nothing is left to
+    // join, where that is no more than kFewKeys.
+    p.waves = !p.shared_rows && s.max_tokens <= kFewKeys && units <= 512 ? 8 : kAttendWaves;
+    const int64_t unit = kAttendStep * p.waves;
+    per = p.waves == 8 ? s.max_tokens
+                       : std::max<int64_t>(per, p.shared_rows ? 4 * unit : 2 * unit);
     p.chunk = (per + unit - 1) / unit * unit;
     p.splits = (s.max_tokens + p.chunk - 1) / p.chunk;
-    p.logit_stride = s.weights ? (s.max_tokens + kAttendStep - 1) / kAttendStep * kAttendStep : 0;
+    p.logit_stride = s.weights ? (s.max_tokens + 63) / 64 * 64 : 0;   // whole steps
     const size_t all = static_cast<size_t>(B * G * p.rows);
     size_t at = 0;
     auto region = [&](size_t floats) {
@@ -268,7 +281,11 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     p.max_off = region(all * parts);
     p.sum_off = region(all * parts);
     p.part_off = region(all * parts * D);
-    p.lse_off = region(s.weights ? all : 0);
+    // Weights take a launch of their own behind rows shared by several workgroups, and behind
+    // a full device, where a workgroup's wait for its last logits would cost more (64
+    // sequences of 32 heads: 85 us in one launch, 73 + 7.5 in two).
+    p.lse_kept = s.weights && (p.shared_rows || (p.splits == 1 && p.waves == kAttendWaves));
+    p.lse_off = region(p.lse_kept ? all : 0);
     p.logit_off = region(all * p.logit_stride);
     p.bytes = at;
     return p;

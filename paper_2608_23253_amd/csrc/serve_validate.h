@@ -30,15 +30,19 @@ inline int elem_bytes(int dtype) { return dtype == E2S_DTYPE_F32 ? 4 : 2; }
 // How an attention call is cut into workgroups, from its sizes alone.
 struct AttendPlan {
     int64_t rows;        // query rows of one key head: H/Hkv * T, row = t * (H/Hkv) + head
-    int tiles;           // 16-row tiles of a workgroup: 1 or 2
+    bool shared_rows;    // the kernel whose waves part the rows (else: the keys)
+    int tiles;           // 16-row tiles of a wave: 1 or 2
+    int waves;           // of a workgroup: kAttendWaves or 8
     int64_t row_groups;  // workgroups along the rows
-    int64_t chunk;       // keys of a workgroup, a multiple of kAttendStep * kAttendWaves
+    int64_t chunk;       // keys of a workgroup, a multiple of kAttendStep * waves
     int64_t splits;      // workgroups along the keys at max_tokens
     int64_t logit_stride;             // floats between the rows of the stored logits
+    bool lse_kept;       // the rows' sums go to the workspace, for the weights' own launch
     size_t max_off, sum_off, part_off, lse_off, logit_off, bytes;   // workspace regions
 };
 constexpr int kAttendWaves = 4;
 constexpr int kAttendStep = 32;     // keys of a wave's step
+constexpr int64_t kFewKeys = 1536;
 AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s);
 
 }  // namespace e2s

@@ -119,7 +119,7 @@ int main() {
                        pl.splits * pl.chunk >= at.max_tokens &&
                        (pl.splits - 1) * pl.chunk < at.max_tokens,
                    "the parts cover the tokens");
-            expect(pl.row_groups * pl.tiles * 16 >= pl.rows, "the row groups cover the rows");
+            expect(pl.row_groups * pl.tiles * (pl.shared_rows ? 64 : 16) >= pl.rows, "the row groups cover the rows");
             expect(pl.max_off <= pl.sum_off && pl.sum_off <= pl.part_off &&
                        pl.part_off <= pl.lse_off && pl.lse_off <= pl.logit_off &&
                        pl.logit_off <= pl.bytes,
