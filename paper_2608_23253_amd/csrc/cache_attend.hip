@@ -91,6 +91,11 @@ __device__ __forceinline__ void split_bf16(float x, __bf16* out) {
     }
 }
 
+// Bits 0, 8, 16 and 24 side by side.
+__device__ __forceinline__ uint32_t gather_bits(uint32_t n) {
+    return (n & 1u) | (n >> 7 & 2u) | (n >> 14 & 4u) | (n >> 21 & 8u);
+}
+
 template <typename T, int N>             // neighbouring elements, stored at once
 struct alignas(N * sizeof(T) < 16 ? N * sizeof(T) : 16) Run { T x[N]; };
 
@@ -194,7 +199,7 @@ struct Step {
 };
 
 template <typename T, int D, int TILES, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, TILES == 1 && WAVES == 4 ? 3 : 2) void attend_kernel(
+__global__ __launch_bounds__(64 * WAVES, TILES == 1 ? 4 : 2) void attend_kernel(
     const AttendArgs a) {
     constexpr int kTerms = Terms<T>::n;
     constexpr int kParts = kTerms < 2 ? 2 : kTerms;      // bf16 terms of a softmax weight
@@ -343,8 +348,10 @@ __global__ __launch_bounds__(64 * WAVES, TILES == 1 && WAVES == 4 ? 3 : 2) void 
 
     f32x4 o[TILES][kDims];
     float top[TILES], base[TILES], sum[TILES];   // running maximum; the same, 0 before any
+    uint32_t poison[TILES];                      // bit 8 r + j: o[.][j][r] is NaN
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
+        poison[t] = 0u;
 #pragma unroll
         for (int j = 0; j < kDims; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         top[t] = -kInf;
@@ -419,20 +426,42 @@ __global__ __launch_bounds__(64 * WAVES, TILES == 1 && WAVES == 4 ? 3 : 2) void 
         const int next = live ? key + kAttendStep : key;
         fetch_k(next, seg, live);
 
-        bool lost = false;                       // a NaN among the values of a masked step
         if constexpr (!kWhole) {
+            // What no row sees may hold anything, and 0 * NaN must not reach the sums.  A NaN
+            // that only some rows see is taken out too and noted for those rows.
+            uint32_t nans[2] = {0u, 0u};         // 8 bits per key, a tile's four keys a word
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int kk = key + (i >> 2) * kTile + 4 * g4 + (i & 3);
                 const bool there = kk < ((i >> 2) ? end1 : end0);
 #pragma unroll
                 for (int h = 0; h < kHalves; ++h) {
-                    // what no row sees may hold anything: 0 * NaN must not reach the sum
-                    if (!there) x.v[i][h] = 0u;
-                    lost = lost || nan_bytes(x.v[i][h]) != 0u;
+                    const uint32_t w = there ? x.v[i][h] : 0u;
+                    const uint32_t n = nan_bytes(w) >> 7;
+                    nans[i >> 2] |= gather_bits(n) << (8 * (i & 3) + 4 * h);
+                    x.v[i][h] = w & ~(n * 0xFFu);
                 }
             }
-            lost = __ballot(lost) != 0;
+            if (__ballot((nans[0] | nans[1]) != 0u)) {
+                // lane (m, g) holds the bits of keys 4 g .. and dimensions m * kDims ..
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+#pragma unroll 1
+                    for (int from = 0; from < 4; ++from) {
+                        const int kk = key + (i >> 2) * kTile + 4 * from + (i & 3);
+                        uint32_t bits = 0;
+#pragma unroll 1
+                        for (int r = 0; r < 4; ++r)
+                            bits |= (static_cast<uint32_t>(
+                                         __shfl(static_cast<int>(nans[i >> 2]),
+                                                from * kTile + 4 * g4 + r)) >> (8 * (i & 3)) &
+                                     0xFFu) << (8 * r);
+#pragma unroll
+                        for (int u = 0; u < TILES; ++u)
+                            if (kk < limit[u]) poison[u] |= bits;
+                    }
+                }
+            }
         }
         bf16x8s pf[TILES][kParts];               // weights as operand columns, in parts
 #pragma unroll
@@ -477,13 +506,7 @@ __global__ __launch_bounds__(64 * WAVES, TILES == 1 && WAVES == 4 ? 3 : 2) void 
             u32x4s vf[4];
 #pragma unroll
             for (int pr = 0; pr < 4; ++pr) {
-                uint32_t wa = x.v[2 * pr][h], wb = x.v[2 * pr + 1][h];
-                if constexpr (!kWhole) {
-                    if (lost) {                  // NaN bytes to 0 here, counted below
-                        wa &= ~((nan_bytes(wa) >> 7) * 0xFFu);
-                        wb &= ~((nan_bytes(wb) >> 7) * 0xFFu);
-                    }
-                }
+                const uint32_t wa = x.v[2 * pr][h], wb = x.v[2 * pr + 1][h];
                 const uint32_t lo = __builtin_amdgcn_perm(wb, wa, 0x05010400u);
                 const uint32_t hi = __builtin_amdgcn_perm(wb, wa, 0x07030602u);
                 const float sc = pr < 2 ? vs0 : vs1;
@@ -501,37 +524,6 @@ __global__ __launch_bounds__(64 * WAVES, TILES == 1 && WAVES == 4 ? 3 : 2) void 
                         o[u][4 * h + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                             __builtin_bit_cast(bf16x8s, vf[j]), pf[u][m], o[u][4 * h + j], 0, 0,
                             0);
-        }
-        if constexpr (!kWhole) {
-            if (lost) {
-                // A NaN value reaches the rows that see its key, and no other: count, per
-                // dimension and row, the seen keys that hold one.
-                bf16x8s seen[TILES];
-#pragma unroll
-                for (int u = 0; u < TILES; ++u)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int kk = key + (i >> 2) * kTile + 4 * g4 + (i & 3);
-                        seen[u][i] = static_cast<__bf16>(kk < limit[u] ? 1.0f : 0.0f);
-                    }
-#pragma unroll
-                for (int j = 0; j < kDims; ++j) {
-                    bf16x8s bad;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        bad[i] = static_cast<__bf16>(
-                            (nan_bytes(x.v[i][j / 4]) >> (8 * (j % 4) + 7)) & 1u ? 1.0f : 0.0f);
-#pragma unroll
-                    for (int u = 0; u < TILES; ++u) {
-                        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-                        const f32x4 hits =
-                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen[u], zero, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (hits[r] > 0.0f) o[u][j][r] = __builtin_nanf("");
-                    }
-                }
-            }
         }
         fetch_v(next, seg, live);
     };
@@ -577,7 +569,8 @@ __global__ __launch_bounds__(64 * WAVES, TILES == 1 && WAVES == 4 ? 3 : 2) void 
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int j = 0; j < kDims; ++j)
-                lds.out[wave][n16][(4 * g4 + r) * kDims + j] = o[u][j][r] * f;
+                lds.out[wave][n16][(4 * g4 + r) * kDims + j] =
+                    poison[u] >> (8 * r + j) & 1u ? __builtin_nanf("") : o[u][j][r] * f;
         __syncthreads();
         constexpr int kPer = kTile * D / (64 * WAVES);   // dimensions per thread: 2 to 8
         const int r = threadIdx.x / (D / kPer), d0 = threadIdx.x % (D / kPer) * kPer;
@@ -651,7 +644,7 @@ struct RowsShared {
     // 16-byte chunk, so that the chunks of one row, written together, lie in different banks
     bf16x8s k[4][D / 32][64];
     u32x2 v[2][D / 16][64][2];           // two halves: 8 bytes of each 16-key tile
-    uint8_t nan[4][kTile][16];           // per key, a bit per dimension: masked steps only
+    alignas(16) uint8_t nan[4][kTile][16];   // per key, a bit per dimension: masked steps only
     int state[4];                        // of each tile: kNoPage, kLost
 };
 constexpr int kNoPage = 1, kLost = 2;    // kLost: a NaN among the values (masked steps)
@@ -718,8 +711,10 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
     }
     f32x4 o[TILES][kDims];
     float top[TILES], base[TILES], sum[TILES];
+    uint32_t poison[TILES];                      // bit 8 r + j: o[.][j][r] is NaN
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
+        poison[u] = 0u;
 #pragma unroll
         for (int j = 0; j < kDims; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         top[u] = -kInf;
@@ -800,8 +795,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
                     for (int h = 0; h < kHalves; ++h) {
                         uint32_t w = in ? x.v[r][h] : 0u;
                         const uint32_t n = nan_bytes(w) >> 7;
-                        bits |= ((n & 1u) | (n >> 7 & 2u) | (n >> 14 & 4u) | (n >> 21 & 8u))
-                                << (4 * h);
+                        bits |= gather_bits(n) << (4 * h);
                         x.v[r][h] = w & ~(n * 0xFFu);
                     }
                     lds.nan[wave][4 * g4 + r][n16] = static_cast<uint8_t>(bits);
@@ -933,31 +927,13 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
         if (lost) {
             // a NaN value reaches the rows that see its key, and no other
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
+            for (int i = 0; i < kRowStep; ++i) {
+                const uint32_t bits =
+                    *reinterpret_cast<const uint32_t*>(&lds.nan[i >> 4][i & 15][4 * g4]);
+                if ((lds.state[i >> 4] & kLost) == 0) continue;    // (not written)
 #pragma unroll
-                for (int j = 0; j < kDims; ++j) {
-                    bf16x8s nans;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        nans[i] = static_cast<__bf16>(
-                            (lds.nan[2 * h + (i >> 2)][4 * g4 + (i & 3)][n16] >> j) & 1
-                                ? 1.0f : 0.0f);
-#pragma unroll
-                    for (int u = 0; u < TILES; ++u) {
-                        bf16x8s seen;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int kk = key + (2 * h + (i >> 2)) * kTile + 4 * g4 + (i & 3);
-                            seen[i] = static_cast<__bf16>(kk < limit[u] ? 1.0f : 0.0f);
-                        }
-                        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-                        const f32x4 hits =
-                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(nans, seen, zero, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (hits[r] > 0.0f) o[u][j][r] = __builtin_nanf("");
-                    }
-                }
+                for (int u = 0; u < TILES; ++u)
+                    if (key + i < limit[u]) poison[u] |= bits;
             }
         }
     }
@@ -966,6 +942,11 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
         const int row = row0 + u * kTile + n16;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < kDims; ++j)
+                if (poison[u] >> (8 * r + j) & 1u) o[u][j][r] = __builtin_nanf("");
         float total = sum[u];
         total += __shfl_xor(total, 16);
         total += __shfl_xor(total, 32);

@@ -207,7 +207,7 @@ e2s_status check_attend(const e2s_cache& c, const e2s_cache_attend_shape* s) {
     const AttendPlan p = attend_plan(c, *s);
     const double heads = static_cast<double>(s->batch) * c.num_kv_heads;
     // every kernel of the call: fewer than 2^32 work-items
-    if (heads * p.row_groups * p.splits * 256.0 >= 4294967296.0 ||
+    if (heads * p.row_groups * p.splits * 64 * p.waves >= 4294967296.0 ||
         heads * (static_cast<double>(p.rows) + (s->max_tokens + 255) / 256) * 256.0 >= 4294967296.0)
         return E2S_ERR_UNSUPPORTED;
     // and a workspace that 63 bits address
