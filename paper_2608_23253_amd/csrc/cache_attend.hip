@@ -164,20 +164,37 @@ __device__ __forceinline__ void weigh(float (&y)[N], float scale, float& top, fl
 __device__ __forceinline__ void token_weights(const AttendArgs& a, int64_t b, int g,
                                               const float* lse, int len, int count, int n0,
                                               int step) {
+    constexpr int kBatch = 4;                    // rows whose loads are under way at once
     const int64_t bg = b * a.G + g;
     const int rows = count * a.group;
     const float* in = a.w_in ? a.w_in + b * a.wi[0] + g * a.wi[1] : nullptr;
     float* out = a.w_out + b * a.wo[0] + g * a.wo[1];
     for (; n0 < len; n0 += step) {
         float w[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int row = 0; row < rows; ++row) {
-            const int limit = seen_by(a, len, count, row / a.group);
-            const float l = lse[row];
-            if (n0 >= limit || l == -kInf) continue;
-            const f32x4 x = *reinterpret_cast<const f32x4*>(
-                a.logits + (bg * a.rows + row) * a.logit_stride + n0);
+        int t = 0, h = 0;                        // of the row whose weight is added next
+        for (int row0 = 0; row0 < rows; row0 += kBatch) {
+            // what a row does not see was not written, and is read but not used
+            f32x4 x[kBatch];
+            float l[kBatch];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] += n0 + i < limit ? exp2_hw(x[i] - l) : 0.0f;
+            for (int j = 0; j < kBatch; ++j) {
+                const int row = min(row0 + j, rows - 1);
+                l[j] = lse[row];
+                x[j] = *reinterpret_cast<const f32x4*>(
+                    a.logits + (bg * a.rows + row) * a.logit_stride + n0);
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (row0 + j >= rows) break;
+                const int limit = l[j] == -kInf ? 0 : seen_by(a, len, count, t);
+                if (++h == a.group) {
+                    h = 0;
+                    ++t;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] += n0 + i < limit ? exp2_hw(x[j][i] - l[j]) : 0.0f;
+            }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -989,35 +1006,60 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
 // key head).  A part is there where its first key is seen by the workgroup that wrote it;
 // parts whose keys this row does not see hold a maximum of -inf.
 template <typename T, int D, int WAVES>
-__device__ __forceinline__ void join_rows(const AttendArgs& a, int64_t block, int64_t lines) {
+__device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block, uint32_t lines) {
     constexpr int kRows = kAttendWaves / WAVES;
     __shared__ float merge[kRows][WAVES][D];
     __shared__ float sums[kRows][WAVES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int which = wave / WAVES, sub = wave % WAVES;
-    const int64_t line = block * kRows + which;
-    const int64_t bg = line < lines ? line / a.rows : 0;
+    const uint32_t line = block * kRows + which;             // < 2^24 + kRows
+    const uint32_t bg = line < lines ? line / static_cast<uint32_t>(a.rows) : 0;
     const int row = static_cast<int>(line - bg * a.rows);
-    const int64_t b = bg / a.G;
-    const int g = static_cast<int>(bg - b * a.G);
+    const int64_t b = bg / static_cast<uint32_t>(a.G);
+    const int g = static_cast<int>(bg - static_cast<uint32_t>(b) * a.G);
     const int len = attend_length(a, b), count = attend_count(a, b);
     const int t = row / a.group;
     const bool live = line < lines && t < count;
     const int limit = live ? seen_by(a, len, count, t) : 0;
-    const int parts = static_cast<int>((limit + a.chunk - 1) / a.chunk);   // <= splits
+    const int parts = (limit + static_cast<int>(a.chunk) - 1) / static_cast<int>(a.chunk);
     constexpr int kPer = D / 64;
-    float m = -kInf;
-    for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.part_max[line * a.splits + i]);
-    m = wave_max(m);
-    float total = 0.0f, y[kPer] = {};
-#pragma unroll 8
-    for (int i = sub; i < parts; i += WAVES) {
-        const int64_t part = line * a.splits + i;
-        const float pm = a.part_max[part];      // -inf: the part holds zeros, or NaN
-        const float f = pm == -kInf ? 1.0f : exp2_hw(pm - m);
-        total += a.part_sum[part] * f;
+    // A lane has the maximum and sum of one of 64 parts; their outputs are read kBatch at a
+    // time, since one after the other each would cost the latency of memory.
+    constexpr int kBatch = WAVES == 1 ? 4 : 8;
+    const int64_t first = static_cast<int64_t>(line) * a.splits;
+    float m = -kInf, total = 0.0f, y[kPer] = {};
+    for (int seg = 0; seg < parts; seg += 64) {
+        const int here = min(parts - seg, 64);
+        const float pm = lane < here ? a.part_max[first + seg + lane] : -kInf;
+        const float ps = lane < here ? a.part_sum[first + seg + lane] : 0.0f;
+        const float up = fmaxf(m, wave_max(pm));
+        const float shrink = up == m ? 1.0f : exp2_hw(m - up);
+        m = up;
+        total *= shrink;
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) y[k] += a.part_out[part * D + lane * kPer + k] * f;
+        for (int k = 0; k < kPer; ++k) y[k] *= shrink;
+        const float f = pm == -kInf ? 1.0f : exp2_hw(pm - up);   // -inf: zeros, or NaN
+        const float sf = ps * f;
+        for (int i0 = sub; i0 < here; i0 += WAVES * kBatch) {
+            float v[kBatch][kPer];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int i = min(i0 + j * WAVES, here - 1);
+                const float* from = a.part_out + (first + seg + i) * D + lane * kPer;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) v[j][k] = from[k];
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int i = i0 + j * WAVES;
+                if (i >= here) break;
+                const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i));
+                total += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sf), i));
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) y[k] += v[j][k] * fi;
+            }
+        }
     }
     if constexpr (WAVES > 1) {
 #pragma unroll
@@ -1073,7 +1115,7 @@ __device__ __forceinline__ void sums_of_parts(const AttendArgs& a, int64_t bg, i
 // weights are wanted and the rows are few, the tokens' weights (`blocks` workgroups to a
 // (sequence, key head), four neighbouring tokens to a thread).
 template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(kThreads) void attend_finish_kernel(const AttendArgs a, int64_t lines,
+__global__ __launch_bounds__(kThreads) void attend_finish_kernel(const AttendArgs a, uint32_t lines,
                                                                  uint32_t joins, uint32_t blocks) {
     if (blockIdx.x < joins) {
         join_rows<T, D, WAVES>(a, blockIdx.x, lines);
@@ -1081,8 +1123,8 @@ __global__ __launch_bounds__(kThreads) void attend_finish_kernel(const AttendArg
     }
     __shared__ float lse[kFewRows];
     const uint32_t id = blockIdx.x - joins;
-    const int64_t bg = id / blocks;
-    const int64_t b = bg / a.G;
+    const uint32_t bg = id / blocks;
+    const int64_t b = bg / static_cast<uint32_t>(a.G);
     const int n0 = static_cast<int>(id % blocks) * 4 * kThreads;
     const int len = attend_length(a, b), count = attend_count(a, b);
     if (n0 >= len) return;
@@ -1094,11 +1136,11 @@ __global__ __launch_bounds__(kThreads) void attend_finish_kernel(const AttendArg
 // The tokens' weights from rows whose sums lie in the workspace.
 __global__ __launch_bounds__(kThreads) void attend_weights_kernel(const AttendArgs a,
                                                                   uint32_t blocks) {
-    const int64_t bg = blockIdx.x / blocks;
-    const int64_t b = bg / a.G;
+    const uint32_t bg = blockIdx.x / blocks;
+    const int64_t b = bg / static_cast<uint32_t>(a.G);
     const int n0 = (static_cast<int>(blockIdx.x % blocks) * kThreads +
                     static_cast<int>(threadIdx.x)) * 4;
-    token_weights(a, b, static_cast<int>(bg - b * a.G), a.lse + bg * a.rows,
+    token_weights(a, b, static_cast<int>(bg - b * a.G), a.lse + static_cast<int64_t>(bg) * a.rows,
                   attend_length(a, b), attend_count(a, b), n0, a.max_tokens);
 }
 
@@ -1125,7 +1167,7 @@ hipError_t launch_t(const AttendArgs& a, const AttendPlan& p, int64_t B, hipStre
     }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    const int64_t lines = B * a.G * a.rows;
+    const uint32_t lines = static_cast<uint32_t>(B * a.G * a.rows);
     const uint32_t blocks = static_cast<uint32_t>((a.max_tokens + 4 * kThreads - 1) /
                                                   (4 * kThreads));
     if (a.splits > 1) {
@@ -1133,12 +1175,11 @@ hipError_t launch_t(const AttendArgs& a, const AttendPlan& p, int64_t B, hipStre
         const uint32_t more =
             a.w_out && !p.lse_kept ? static_cast<uint32_t>(B * a.G) * blocks : 0u;
         if (a.splits > 8) {
-            const uint32_t joins = static_cast<uint32_t>(lines);
+            const uint32_t joins = lines;
             hipLaunchKernelGGL((attend_finish_kernel<T, D, kAttendWaves>), dim3(joins + more),
                                block, 0, st, a, lines, joins, blocks);
         } else {
-            const uint32_t joins =
-                static_cast<uint32_t>((lines + kAttendWaves - 1) / kAttendWaves);
+            const uint32_t joins = (lines + kAttendWaves - 1) / kAttendWaves;
             hipLaunchKernelGGL((attend_finish_kernel<T, D, 1>), dim3(joins + more), block, 0, st,
                                a, lines, joins, blocks);
         }

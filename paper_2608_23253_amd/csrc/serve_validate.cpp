@@ -259,8 +259,13 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
         p.tiles = 1;
     p.row_groups = (p.rows + per_tile * p.tiles - 1) / (per_tile * p.tiles);
     const int64_t units = B * G * p.row_groups;
-    const int64_t want = p.shared_rows ? 1536 : 2048;   // workgroups that fill the device
-    int64_t per = (s.max_tokens * units + want - 1) / want;
+    // Keys are split until 2048 workgroups fill the device, most of which have nothing to do
+    // where sequences are of unequal lengths (16 of 300 to 4200 keys, up to 48 queries of 28
+    // heads: 60 us; 1536 workgroups: 74, 3072: 63).  Units of 32 rows to a wave are enough as
+    // they are: 4 sequences of 512 queries and 2000 keys, 32 heads take 121 us unsplit, 169
+    // and 178 in two and three parts.
+    int64_t per = p.shared_rows && p.tiles == 2 ? s.max_tokens
+                                                : (s.max_tokens * units + 2047) / 2048;
     // Short sequences: one workgroup of eight waves has all keys, and nothing is left to
     // join, where that is no more than kFewKeys.
     p.waves = !p.shared_rows && s.max_tokens <= kFewKeys && units <= 512 ? 8 : kAttendWaves;
