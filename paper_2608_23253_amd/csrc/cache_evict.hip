@@ -3,7 +3,8 @@
 // evict_select_kernel, one workgroup per (sequence, key head): the tokens between the
 // first `sinks` and the last `recent` are ranked by a 32-bit key that orders floats as
 // integers (larger weight, larger key; NaN lowest), and the want-th largest key is found
-// digit by digit (11, 11 and 10 bits) from a histogram in LDS.  Tokens above it stay, and
+// digit by digit (11, 11 and 10 bits) from a histogram in LDS, until all tokens that share
+// the digits found so far stay.  Tokens above it stay, and
 // of those equal to it the first ones; counts per wave and a scan over the waves place the
 // kept tokens in ascending order.  All decisions are on integers, so nothing depends on
 // the order of the atomic increments.  Latency bounds it: a thread loads its keys (up to 16)
@@ -52,12 +53,18 @@ __device__ __forceinline__ uint32_t rank_key(float w) {
     return w != w ? 0u : ordered_bits(w + 0.0f);
 }
 
+// How many of the lanes before this one a ballot names.
+__device__ __forceinline__ uint32_t lanes_below(uint64_t ballot) {
+    return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(ballot >> 32),
+                                     __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(ballot), 0u));
+}
+
 template <int PER>                       // tokens per thread and segment
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
     __shared__ uint32_t hist[kBins];
     __shared__ uint32_t sums[kSelWaves];
     __shared__ uint32_t ties[kSelWaves];
-    __shared__ uint32_t found[2];
+    __shared__ uint32_t found[3];             // digit, still wanted, of how many
     constexpr int kSegment = kSelThreads * PER;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -83,6 +90,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
     const int m0 = a.sinks, m1 = n - a.recent;
     // A wave holds PER runs of 64 neighbouring tokens of a segment, one after the other.
     float x[PER];
+    uint32_t key[PER];
     auto token = [&](int seg, int j) { return seg + (wave * PER + j) * kWave + lane; };
     auto load = [&](int seg) {
 #pragma unroll
@@ -90,7 +98,11 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
             const int i = token(seg, j);
             x[j] = i < n ? w[i] : 0.0f;
         }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = rank_key(x[j]);
     };
+    const uint32_t between = static_cast<uint32_t>(m1 - m0);
+    auto ranked = [&](int i) { return static_cast<uint32_t>(i - m0) < between; };
     const bool once = n <= kSegment;
     if (once) load(0);
     uint32_t want = static_cast<uint32_t>(a.K - a.sinks - a.recent);
@@ -110,10 +122,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
                 if (!once) load(seg);
 #pragma unroll
                 for (int j = 0; j < PER; ++j) {
-                    const int i = token(seg, j);
-                    const uint32_t key = rank_key(x[j]);
-                    if (i >= m0 && i < m1 && (key & known) == limit)
-                        atomicAdd(&hist[(key >> shift) & mask], 1u);
+                    if (ranked(token(seg, j)) && (key[j] & known) == limit)
+                        atomicAdd(&hist[(key[j] >> shift) & mask], 1u);
                 }
             }
             __syncthreads();
@@ -134,28 +144,33 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
                 const bool upper = above + h1 >= want;
                 found[0] = static_cast<uint32_t>(kBins - 1 - 2 * tid - (upper ? 0 : 1));
                 found[1] = want - above - (upper ? 0 : h1);
+                found[2] = upper ? h1 : h0;
             }
             __syncthreads();
             limit |= found[0] << shift;
             want = found[1];
             known |= mask << shift;
+            if (found[2] == want && limit > 0) {       // all that share the digits stay
+                --limit;
+                want = 0;
+                break;
+            }
         }
     }
     // Per segment: every wave counts its tokens that stay and its ties, then places them.
     uint32_t more = 0, same = 0;                       // of the segments before
     for (int seg = 0; seg < n; seg += kSegment) {
         if (!once) load(seg);
-        uint64_t ups[PER], equal[PER];
+        bool up[PER], equal[PER];
         uint32_t up_here = 0, tie_here = 0;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int i = token(seg, j);
-            const uint32_t key = rank_key(x[j]);
-            const bool end = i < m0 || i >= m1;
-            ups[j] = __ballot(i < n && (end || key > limit));
-            equal[j] = __ballot(i < n && !end && key == limit);
-            up_here += __popcll(ups[j]);
-            tie_here += __popcll(equal[j]);
+            const bool inner = ranked(i);
+            up[j] = i < n && (!inner || key[j] > limit);
+            equal[j] = inner && key[j] == limit;
+            up_here += __popcll(__ballot(up[j]));
+            tie_here += __popcll(__ballot(equal[j]));
         }
         __syncthreads();                               // sums and ties are free
         if (lane == 0) {
@@ -173,16 +188,15 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
         }
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            const uint64_t below = (uint64_t{1} << lane) - 1;
-            const uint32_t tie = before + __popcll(equal[j] & below);
-            const bool stays = (ups[j] >> lane & 1) || ((equal[j] >> lane & 1) && tie < want);
-            if (stays) {                               // K tokens in all, so slot < K
-                const uint32_t slot = slot0 + __popcll(ups[j] & below) + min(tie, want);
+            const uint64_t ups = __ballot(up[j]), ties_here = __ballot(equal[j]);
+            const uint32_t tie = before + lanes_below(ties_here);
+            if (up[j] || (equal[j] && tie < want)) {   // K tokens in all, so slot < K
+                const uint32_t slot = slot0 + lanes_below(ups) + min(tie, want);
                 keep[slot] = token(seg, j);
                 if (left) left[slot] = x[j];
             }
-            slot0 += __popcll(ups[j]);
-            before += __popcll(equal[j]);
+            slot0 += __popcll(ups);
+            before += __popcll(ties_here);
         }
     }
 }
