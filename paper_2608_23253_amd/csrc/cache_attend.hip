@@ -1001,58 +1001,120 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
     }
 }
 
-// Joins the parts of a row, WAVES waves to a row (several where the parts are many, and
-// reading them one after the other would take long); `line` counts rows over all (sequence,
-// key head).  A part is there where its first key is seen by the workgroup that wrote it;
-// parts whose keys this row does not see hold a maximum of -inf.
-template <typename T, int D, int WAVES>
-__device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block, uint32_t lines) {
-    constexpr int kRows = kAttendWaves / WAVES;
-    __shared__ float merge[kRows][WAVES][D];
-    __shared__ float sums[kRows][WAVES];
+// The parts of a row that were written: a part is there where its first key is seen by the
+// workgroup that wrote it; parts whose keys this row does not see hold a maximum of -inf (and
+// zeros, or NaN).
+struct JoinRow {
+    int64_t b, first;                            // sequence; the row's first part
+    int g, head, t, parts;
+    bool live;
+};
+__device__ __forceinline__ JoinRow join_row(const AttendArgs& a, uint32_t line, uint32_t lines) {
+    JoinRow r;
+    const uint32_t bg = line < lines ? line / static_cast<uint32_t>(a.rows) : 0;
+    const uint32_t row = line - bg * static_cast<uint32_t>(a.rows);
+    r.b = bg / static_cast<uint32_t>(a.G);
+    r.g = static_cast<int>(bg - static_cast<uint32_t>(r.b) * a.G);
+    r.t = static_cast<int>(row / static_cast<uint32_t>(a.group));
+    r.head = r.g * a.group + static_cast<int>(row) - r.t * a.group;
+    const int len = attend_length(a, r.b), count = attend_count(a, r.b);
+    r.live = line < lines && r.t < count;
+    const int chunk = static_cast<int>(a.chunk);
+    r.parts = r.live ? (seen_by(a, len, count, r.t) + chunk - 1) / chunk : 0;   // <= splits
+    r.first = static_cast<int64_t>(line) * a.splits;
+    return r;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void join_out(const AttendArgs& a, const JoinRow& r, uint32_t line,
+                                         int dim, float m, float total, const float (&y)[N]) {
+    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+    T* to = static_cast<T*>(a.out) + r.b * a.os[0] + r.head * a.os[1] + r.t * a.os[2] + dim;
+    Run<T, N> z;
+#pragma unroll
+    for (int k = 0; k < N; ++k) z.x[k] = from_f32<T>(y[k] * inv);
+    *reinterpret_cast<Run<T, N>*>(to) = z;
+    if (a.lse && dim == 0)
+        a.lse[line] = total > 0.0f || total != total ? m + __log2f(total) : -kInf;
+}
+
+// Joins few parts (<= kFewParts), four dimensions to a thread: every thread reads the maxima
+// and sums of its row itself, so all that it needs is under way at once.
+constexpr int kFewParts = 8;
+template <typename T, int D>
+__device__ __forceinline__ void join_few(const AttendArgs& a, uint32_t block, uint32_t lines) {
+    constexpr int kLanes = D / 4, kBatch = 4;
+    const uint32_t line = block * (kThreads / kLanes) + threadIdx.x / kLanes;   // < 2^24 + 16
+    const int dim = static_cast<int>(threadIdx.x) % kLanes * 4;
+    const JoinRow r = join_row(a, line, lines);
+    if (!r.live) return;
+    float m = -kInf, total = 0.0f, y[4] = {};
+    for (int i0 = 0; i0 < r.parts; i0 += kBatch) {
+        float pm[kBatch], ps[kBatch];
+        f32x4 v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t part = r.first + min(i0 + j, r.parts - 1);
+            pm[j] = a.part_max[part];
+            ps[j] = a.part_sum[part];
+            v[j] = *reinterpret_cast<const f32x4*>(a.part_out + part * D + dim);
+        }
+        float up = m;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) up = fmaxf(up, pm[j]);
+        const float shrink = up == m ? 1.0f : exp2_hw(m - up);
+        m = up;
+        total *= shrink;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] *= shrink;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (i0 + j >= r.parts) break;
+            const float f = pm[j] == -kInf ? 1.0f : exp2_hw(pm[j] - up);
+            total += ps[j] * f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] += v[j][k] * f;
+        }
+    }
+    join_out<T>(a, r, line, dim, m, total, y);
+}
+
+// Joins many parts, a workgroup to a row: a lane has the maximum and sum of one of 64 parts,
+// and the waves share the outputs, each reading kBatch at a time.
+template <typename T, int D>
+__device__ __forceinline__ void join_many(const AttendArgs& a, uint32_t line, uint32_t lines) {
+    constexpr int kPer = D / 64, kBatch = 8;
+    __shared__ float merge[kAttendWaves][D];
+    __shared__ float sums[kAttendWaves];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int which = wave / WAVES, sub = wave % WAVES;
-    const uint32_t line = block * kRows + which;             // < 2^24 + kRows
-    const uint32_t bg = line < lines ? line / static_cast<uint32_t>(a.rows) : 0;
-    const int row = static_cast<int>(line - bg * a.rows);
-    const int64_t b = bg / static_cast<uint32_t>(a.G);
-    const int g = static_cast<int>(bg - static_cast<uint32_t>(b) * a.G);
-    const int len = attend_length(a, b), count = attend_count(a, b);
-    const int t = row / a.group;
-    const bool live = line < lines && t < count;
-    const int limit = live ? seen_by(a, len, count, t) : 0;
-    const int parts = (limit + static_cast<int>(a.chunk) - 1) / static_cast<int>(a.chunk);
-    constexpr int kPer = D / 64;
-    // A lane has the maximum and sum of one of 64 parts; their outputs are read kBatch at a
-    // time, since one after the other each would cost the latency of memory.
-    constexpr int kBatch = WAVES == 1 ? 4 : 8;
-    const int64_t first = static_cast<int64_t>(line) * a.splits;
+    const JoinRow r = join_row(a, line, lines);
+    if (!r.live) return;                         // all threads
     float m = -kInf, total = 0.0f, y[kPer] = {};
-    for (int seg = 0; seg < parts; seg += 64) {
-        const int here = min(parts - seg, 64);
-        const float pm = lane < here ? a.part_max[first + seg + lane] : -kInf;
-        const float ps = lane < here ? a.part_sum[first + seg + lane] : 0.0f;
+    for (int seg = 0; seg < r.parts; seg += 64) {
+        const int here = min(r.parts - seg, 64);
+        const float pm = lane < here ? a.part_max[r.first + seg + lane] : -kInf;
+        const float ps = lane < here ? a.part_sum[r.first + seg + lane] : 0.0f;
         const float up = fmaxf(m, wave_max(pm));
         const float shrink = up == m ? 1.0f : exp2_hw(m - up);
         m = up;
         total *= shrink;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) y[k] *= shrink;
-        const float f = pm == -kInf ? 1.0f : exp2_hw(pm - up);   // -inf: zeros, or NaN
+        const float f = pm == -kInf ? 1.0f : exp2_hw(pm - up);
         const float sf = ps * f;
-        for (int i0 = sub; i0 < here; i0 += WAVES * kBatch) {
+        for (int i0 = wave; i0 < here; i0 += kAttendWaves * kBatch) {
             float v[kBatch][kPer];
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
-                const int i = min(i0 + j * WAVES, here - 1);
-                const float* from = a.part_out + (first + seg + i) * D + lane * kPer;
+                const int i = min(i0 + j * kAttendWaves, here - 1);
+                const float* from = a.part_out + (r.first + seg + i) * D + lane * kPer;
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) v[j][k] = from[k];
             }
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
-                const int i = i0 + j * WAVES;
+                const int i = i0 + j * kAttendWaves;
                 if (i >= here) break;
                 const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i));
                 total += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sf), i));
@@ -1061,31 +1123,18 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block, u
             }
         }
     }
-    if constexpr (WAVES > 1) {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) merge[which][sub][lane * kPer + k] = y[k];
-        if (lane == 0) sums[which][sub] = total;
-        __syncthreads();
-        total = sums[which][0];
+    for (int k = 0; k < kPer; ++k) merge[wave][lane * kPer + k] = y[k];
+    if (lane == 0) sums[wave] = total;
+    __syncthreads();
+    if (wave != 0) return;
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) y[k] = merge[which][0][lane * kPer + k];
+    for (int w = 1; w < kAttendWaves; ++w) {
+        total += sums[w];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) {
-            total += sums[which][w];
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) y[k] += merge[which][w][lane * kPer + k];
-        }
+        for (int k = 0; k < kPer; ++k) y[k] += merge[w][lane * kPer + k];
     }
-    if (!live || sub != 0) return;
-    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-    T* to = static_cast<T*>(a.out) + b * a.os[0] + (g * a.group + row - t * a.group) * a.os[1] +
-            t * a.os[2] + lane * kPer;
-    Run<T, kPer> z;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) z.x[k] = from_f32<T>(y[k] * inv);
-    *reinterpret_cast<Run<T, kPer>*>(to) = z;
-    if (a.lse && lane == 0)
-        a.lse[line] = total > 0.0f || total != total ? m + __log2f(total) : -kInf;
+    join_out<T>(a, r, line, lane * kPer, m, total, y);
 }
 
 // log2 of the sums of up to kFewRows rows, from their parts, into LDS: a wave to a row.
@@ -1114,11 +1163,12 @@ __device__ __forceinline__ void sums_of_parts(const AttendArgs& a, int64_t bg, i
 // What is left after the parts: the rows' joins (the first `joins` workgroups) and, where
 // weights are wanted and the rows are few, the tokens' weights (`blocks` workgroups to a
 // (sequence, key head), four neighbouring tokens to a thread).
-template <typename T, int D, int WAVES>
+template <typename T, int D, bool MANY>
 __global__ __launch_bounds__(kThreads) void attend_finish_kernel(const AttendArgs a, uint32_t lines,
                                                                  uint32_t joins, uint32_t blocks) {
     if (blockIdx.x < joins) {
-        join_rows<T, D, WAVES>(a, blockIdx.x, lines);
+        if constexpr (MANY) join_many<T, D>(a, blockIdx.x, lines);
+        else join_few<T, D>(a, blockIdx.x, lines);
         return;
     }
     __shared__ float lse[kFewRows];
@@ -1174,13 +1224,13 @@ hipError_t launch_t(const AttendArgs& a, const AttendPlan& p, int64_t B, hipStre
         // the weights of few rows in the same launch
         const uint32_t more =
             a.w_out && !p.lse_kept ? static_cast<uint32_t>(B * a.G) * blocks : 0u;
-        if (a.splits > 8) {
+        if (a.splits > kFewParts) {
             const uint32_t joins = lines;
-            hipLaunchKernelGGL((attend_finish_kernel<T, D, kAttendWaves>), dim3(joins + more),
+            hipLaunchKernelGGL((attend_finish_kernel<T, D, true>), dim3(joins + more),
                                block, 0, st, a, lines, joins, blocks);
         } else {
-            const uint32_t joins = (lines + kAttendWaves - 1) / kAttendWaves;
-            hipLaunchKernelGGL((attend_finish_kernel<T, D, 1>), dim3(joins + more), block, 0, st,
+            const uint32_t per = kThreads / (D / 4), joins = (lines + per - 1) / per;
+            hipLaunchKernelGGL((attend_finish_kernel<T, D, false>), dim3(joins + more), block, 0, st,
                                a, lines, joins, blocks);
         }
         err = hipGetLastError();
