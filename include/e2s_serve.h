@@ -21,6 +21,7 @@
  * Shape symbols: B sequences, H query heads, Hkv key heads (query head h reads key head
  * floor(h*Hkv/H)), T new tokens or queries per sequence, d head_dim, P tokens per page.
  * Strides count elements; a row (the d elements of one token and head) is contiguous.
+ * An output overlaps neither an input nor another output unless its call says that it may.
  */
 #ifndef E2S_SERVE_H
 #define E2S_SERVE_H
@@ -171,7 +172,7 @@ typedef struct {
     int32_t causal;         /* 1: the queries are the sequence's last tokens; 0: every
                                query sees all                                         */
     int32_t weights;        /* 1: weights_out is given; sizes the workspace           */
-    float scale;            /* logit scale, finite, >= 0; 0 selects 1/sqrt(d)         */
+    float scale;            /* logit scale, 0 .. 2e38; 0 selects 1/sqrt(d)            */
     int32_t reserved;       /* 0                                                      */
     int64_t pages_stride;
     int64_t q_stride[3];    /* sequence, head, query                                  */
@@ -195,9 +196,10 @@ E2S_API e2s_status e2s_cache_attend_workspace_size(const e2s_cache* cache,
  *   weights_out_opt [B, Hkv, >= max_tokens] f32 or NULL: for n < len, weights_in[b, h, n]
  *            (0 where weights_in_opt is NULL) plus the softmax weight of token n summed
  *            over the queries and the query heads of key head h, in a fixed order;
- *            entries from len on are left as they were.  It may be weights_in itself.
+ *            entries from len on are left as they were.  It may be weights_in itself,
+ *            with its strides.
  * Logits, maxima, sums and the output accumulate in 32 bits; the weights that multiply
- * the values are rounded to 8 (bf16 q), 16 (f16) or 24 bits (f32).
+ * the values are rounded to 16 bits (bf16 and f16 q) or 24 bits (f32).
  * workspace: 256-byte aligned, >= e2s_cache_attend_workspace_size bytes (NULL if 0),
  * contents undefined on return.  A NaN in a held key or value reaches the queries that
  * see it and no other. */
@@ -223,7 +225,7 @@ typedef struct {
  * token; NaN after all others), in their order.
  *   weights   [B, Hkv, >= max_tokens] f32
  *   keep_idx  [B, Hkv, K] int32 out: the kept tokens, ascending, then -1
- *   new_len   [B] int32 out: min(len, K)
+ *   new_len   [B] int32 out: min(len, K); not lengths itself
  *   weights_left_opt [B, Hkv, W] f32 out or NULL: the kept tokens' weights, then zeros
  * The kept rows go to the pages of new_pages [B, new_max_pages], which must not be among
  * the sequences' present pages; each new block gets its own scale.  A kept row whose page

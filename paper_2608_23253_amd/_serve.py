@@ -9,6 +9,7 @@ status.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -100,6 +101,17 @@ _ROTARY = struct.Struct("@6i15q")
 _APPEND = struct.Struct("@6i7q")
 _ATTEND = struct.Struct("@8ifi11q")
 _EVICT = struct.Struct("@8i6q")
+
+
+def _allocating_on(stream, device):
+    """What a call allocates, and fills with zeros, belongs to the stream it runs on."""
+    if stream is None:
+        return _HERE
+    torch = _torch()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device))
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _rows(t, name, dtype=None):
@@ -250,8 +262,8 @@ class PagedCache:
         torch = _torch()
         for t, name in ((k, "k"), (v, "v")):
             _check(t, name, dtype=torch.float8_e4m3fn, ndim=4, contiguous=False)
-            if t.shape != k.shape:
-                raise ValueError("k and v must have one shape [num_pages, Hkv, P, d]")
+            if t.shape != k.shape or t.numel() == 0:
+                raise ValueError("k and v must have one shape [num_pages, Hkv, P, d], not empty")
             if not t[0].is_contiguous():
                 raise ValueError(f"a page of {name} must be contiguous")
         for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
@@ -350,7 +362,8 @@ class CacheAttention:
         lengths_at = _vector(lengths, "lengths", self.batch)
         count_at = None if q_count is None else _vector(q_count, "q_count", self.batch)
         if out is None:
-            out = torch.empty_like(q) if q_count is None else torch.zeros_like(q)
+            with _allocating_on(stream, q.device):
+                out = torch.empty_like(q) if q_count is None else torch.zeros_like(q)
             os_ = out.stride()
         else:
             os_ = _rows(out, "out", self.dtype)
@@ -359,8 +372,9 @@ class CacheAttention:
         wi = wo = (0, 0)
         if self.weights:
             if weights_out is None:
-                weights_out = torch.zeros(self._w_shape + (self.max_tokens,), device=q.device,
-                                          dtype=torch.float32)
+                with _allocating_on(stream, q.device):
+                    weights_out = torch.zeros(self._w_shape + (self.max_tokens,),
+                                              device=q.device, dtype=torch.float32)
             wo = self._weights(weights_out, "weights_out")
             if weights_in is not None:
                 wi = self._weights(weights_in, "weights_in")
@@ -381,6 +395,7 @@ def cache_attend(q, cache: PagedCache, pages, lengths, max_tokens: Optional[int]
     """One CacheAttention call: (out, weights or None).  max_tokens: no length is larger
     (default: what the page table can hold)."""
     _rows(q, "q")
+    _table(pages, "pages", q.shape[0])
     if max_tokens is None:
         max_tokens = pages.shape[1] * cache.page_tokens
     weights = want_weights or weights_in is not None or weights_out is not None
@@ -409,19 +424,19 @@ def cache_evict(cache: PagedCache, pages, lengths, weights, new_pages, budget: i
     new_width, new_row = _table(new_pages, "new_pages", B)
     lengths_at = _vector(lengths, "lengths", B)
     K = max(budget, 0)
-    keep, kept = lengths.new_empty((B, G, K)), torch.empty_like(lengths)
-    if weights_left is None:
-        weights_left = weights.new_empty((B, G, K))
-    else:
+    with _allocating_on(stream, weights.device):
+        keep, kept = lengths.new_empty((B, G, K)), torch.empty_like(lengths)
+        left = weights.new_empty((B, G, K)) if weights_left is None else weights_left
+    if weights_left is not None:
         _check(weights_left, "weights_left", dtype=torch.float32, ndim=3, contiguous=False)
         if tuple(weights_left.shape[:2]) != (B, G) or \
                 (weights_left.stride(2) != 1 and weights_left.shape[2] > 1):
             raise ValueError(f"weights_left must be [{B}, {G}, >= budget] with contiguous rows")
-    sh = _EVICT.pack(B, N, budget, sinks, recent, width, new_width, weights_left.shape[2], row,
-                     new_row, *ws[:2], *weights_left.stride()[:2])
+    sh = _EVICT.pack(B, N, budget, sinks, recent, width, new_width, left.shape[2], row,
+                     new_row, *ws[:2], *left.stride()[:2])
     _launch("e2s_cache_evict",
-            (cache.k, pages, lengths, weights, new_pages, keep, kept, weights_left),
+            (cache.k, pages, lengths, weights, new_pages, keep, kept, left),
             _LIB.e2s_cache_evict, cache.desc_ref, sh, pages.data_ptr(), lengths_at,
             weights.data_ptr(), new_pages.data_ptr(), keep.data_ptr(), kept.data_ptr(),
-            weights_left.data_ptr(), stream=stream)
-    return keep, kept, weights_left
+            left.data_ptr(), stream=stream)
+    return keep, kept, left

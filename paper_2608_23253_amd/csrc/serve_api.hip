@@ -1,5 +1,7 @@
 // extern "C" entry points of e2s_serve.h.  Each call validates every argument on the host
 // before it touches the HIP runtime, then enqueues its kernels on the caller's stream.
+#include <initializer_list>
+
 #include "e2s_serve.h"
 #include "serve_kernels.h"
 
@@ -18,6 +20,19 @@ e2s_status need(const void* p, size_t a) {
     return p ? e2s::check_aligned(p, a) : E2S_ERR_NULL_POINTER;
 }
 e2s_status optional(const void* p, size_t a) { return p ? e2s::check_aligned(p, a) : E2S_OK; }
+
+// An output in its input's place has the input's strides (where a dimension has more than one
+// index): with others it would write what is still to be read.
+e2s_status in_place(const void* in, const void* out, const int64_t* is, const int64_t* os,
+                    std::initializer_list<int64_t> counts) {
+    if (in != out || in == nullptr) return E2S_OK;
+    int i = 0;
+    for (const int64_t n : counts) {
+        if (n > 1 && is[i] != os[i]) return E2S_ERR_BAD_PARAM;
+        ++i;
+    }
+    return E2S_OK;
+}
 
 }  // namespace
 
@@ -43,10 +58,14 @@ e2s_status e2s_rotate_positions(const e2s_rotary_shape* shape, const e2s_rotary_
     if (shape->q_heads > 0) {
         E2S_TRY(need(q, eb));
         E2S_TRY(need(q_out, eb));
+        E2S_TRY(in_place(q, q_out, shape->q_stride, shape->q_out_stride,
+                         {shape->batch, shape->q_heads, shape->num_tokens}));
     }
     if (shape->k_heads > 0) {
         E2S_TRY(need(k, eb));
         E2S_TRY(need(k_out, eb));
+        E2S_TRY(in_place(k, k_out, shape->k_stride, shape->k_out_stride,
+                         {shape->batch, shape->k_heads, shape->num_tokens}));
     }
     return from_hip(e2s::launch_rotate(*shape, *plan, positions, q, k, q_out, k_out,
                                        static_cast<hipStream_t>(stream)));
@@ -96,6 +115,8 @@ e2s_status e2s_cache_attend(const e2s_cache* cache, const e2s_cache_attend_shape
     if (weights_in_opt != nullptr && weights_out_opt == nullptr) return E2S_ERR_BAD_PARAM;
     E2S_TRY(optional(weights_in_opt, 4));
     E2S_TRY(optional(weights_out_opt, 4));
+    E2S_TRY(in_place(weights_in_opt, weights_out_opt, shape->weights_in_stride,
+                     shape->weights_out_stride, {shape->batch, cache->num_kv_heads}));
     const size_t bytes = e2s::attend_plan(*cache, *shape).bytes;
     if (bytes > 0) E2S_TRY(need(workspace, 256));
     if (workspace_bytes < bytes) return E2S_ERR_WORKSPACE_TOO_SMALL;
@@ -121,6 +142,8 @@ e2s_status e2s_cache_evict(const e2s_cache* cache, const e2s_cache_evict_shape* 
     if (new_pages == pages) return E2S_ERR_BAD_PARAM;
     // the selection reads the weights several times while it writes the kept ones
     if (weights_left_opt == weights) return E2S_ERR_BAD_PARAM;
+    // one key head's workgroup writes the new length while others read the old one
+    if (new_len == lengths) return E2S_ERR_BAD_PARAM;
     return from_hip(e2s::launch_cache_evict(*cache, *shape, pages, lengths, weights, new_pages,
                                             keep_idx, new_len, weights_left_opt,
                                             static_cast<hipStream_t>(stream)));

@@ -567,3 +567,31 @@ def test_on_another_stream():
         got, _ = E.cache_attend(q, cache, pages, lengths)
     s.synchronize()
     assert torch.equal(got, want)
+
+
+def test_on_a_given_stream():
+    """`stream` without entering it: what the calls allocate and fill belongs to it."""
+    rng = np.random.default_rng(43)
+    pool, table = _filled(rng, [500, 90], 2, 32, 128, spare=4)
+    q = torch.from_numpy(rng.standard_normal((2, 4, 3, 128))).to(BF).cuda()
+    cache = E.PagedCache.of(*pool.tensors())
+    free = [p for p in range(pool.k.shape[0]) if p not in set(table.ravel().tolist())]
+    fresh = _cuda(np.array(free[:4], np.int32).reshape(2, 2))
+    pages, lengths, counts = _cuda(table), _ints([500, 90]), _ints([3, 1])
+    att = E.CacheAttention(cache, 2, 4, 3, 512, weights=True)
+    out, w = att(q, pages, lengths, q_count=counts)
+    keep, kept, left = E.cache_evict(cache, pages, lengths, w, fresh, 40, 2, 5)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    out2, w2 = att(q, pages, lengths, q_count=counts, stream=s.cuda_stream)
+    s.synchronize()
+    k2, n2, left2 = E.cache_evict(cache, pages, lengths, w2, fresh, 40, 2, 5,
+                                  stream=s.cuda_stream)
+    s.synchronize()
+    for a, b in ((out, out2), (w, w2), (keep, k2), (kept, n2), (left, left2)):
+        assert torch.equal(a, b)
+
+
+def test_no_empty_cache():
+    with pytest.raises(ValueError):
+        E.PagedCache(0, 2, 64, 16)

@@ -316,6 +316,17 @@ def test_evict_refusals():
         assert evict(**kw) == L.ERR_MISALIGNED, kw
 
 
+def test_in_place_only_with_the_same_strides():
+    """Refused before anything is enqueued: an output in its input's place, laid out
+    otherwise, and the new lengths in the old ones' place."""
+    assert rotate(qo=A, q_out_stride=(1280, 64, 256)) == L.ERR_BAD_PARAM
+    assert rotate(ko=A, k_out_stride=(640, 64, 128)) == L.ERR_BAD_PARAM
+    for strides in ((300, 100), (200, 101)):
+        assert attend(weights=1, win=A, wout=A, weights_out_stride=strides) == L.ERR_BAD_PARAM
+    assert attend(scale=3e38) == L.ERR_BAD_PARAM
+    assert evict(lengths=3 * A, kept=3 * A) == L.ERR_BAD_PARAM
+
+
 def test_validation_under_asan_and_ubsan(tmp_path):
     """serve_validate.cpp on random, often extreme, arguments."""
     if shutil.which("g++") is None:
@@ -352,3 +363,5 @@ def test_binding_refuses_cpu_tensors_and_wrong_types():
                         *[torch.zeros((2, 1))] * 2)
     with pytest.raises(ValueError):
         S.PagedCache(2, 1, 64, 16, device="cpu")
+    with pytest.raises(ValueError):
+        S.cache_attend(x, None, None, None)
