@@ -249,8 +249,12 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     const int64_t B = s.batch, G = c.num_kv_heads, D = c.head_dim;
     p.rows = static_cast<int64_t>(s.num_heads) / G * s.num_queries;
     // Up to 32 rows, a workgroup's waves share the rows and part the keys; above, they part
-    // the rows (16 or 32 each) and share the keys' operands in LDS.
-    p.shared_rows = p.rows > 32;
+    // the rows (16 or 32 each) and share the keys' operands in LDS.  Two tiles of rows keep a
+    // wave that parts the keys busy with products, so from 17 rows on the rows are parted where
+    // there are many keys, although half of the waves then have none: 4 queries of 28 heads
+    // (4 key heads) against 4 sequences of 16000 keys take 27 us so and 35 us, of 2000 keys 18
+    // and 15.
+    p.shared_rows = p.rows > 32 || (p.rows > 16 && B * G * s.max_tokens > 131072);
     const int64_t per_tile = p.shared_rows ? 16 * kAttendWaves : 16;
     p.tiles = p.rows <= per_tile ? 1 : 2;
     // 32 rows to a wave halve what is widened and read from LDS per row, where that still
@@ -268,12 +272,27 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     // and 178 in two and three parts.
     int64_t per = p.shared_rows && p.tiles == 2 ? s.max_tokens
                                                 : (s.max_tokens * units + 2047) / 2048;
-    // Short sequences: one workgroup of eight waves has all keys, and nothing is left to
-    // join, where that is no more than kFewKeys.
-    p.waves = !p.shared_rows && s.max_tokens <= kFewKeys && units <= 512 ? 8 : kAttendWaves;
+    // Short sequences: one workgroup of eight waves has all keys, and nothing is left to join.
+    // With few units that pays up to kFewKeys keys (one sequence, 4 key heads: 512 keys 7.8 us
+    // and 8.9 in parts, 1024 keys 10.4 and 9.4), with more of them up to kShortKeys (32 of 2000
+    // keys, 8 key heads: 25 us and 32; 64 of 1024: 24 and 31), until workgroups of four waves
+    // fill the device unsplit (200 of 300 keys: 35 us and 25).
+    p.waves = !p.shared_rows && units < 1024 &&
+                      s.max_tokens <= (units < 128 ? kFewKeys : kShortKeys)
+                  ? 8
+                  : kAttendWaves;
     const int64_t unit = kAttendStep * p.waves;
-    per = p.waves == 8 ? s.max_tokens
-                       : std::max<int64_t>(per, p.shared_rows ? 4 * unit : 2 * unit);
+    if (p.waves == 8) {
+        per = s.max_tokens;
+    } else if (p.shared_rows) {
+        per = std::max<int64_t>(per, 4 * unit);
+    } else {
+        // Parts of fewer than 1024 keys are mostly their own beginning and end: there 1024
+        // workgroups are enough (200 sequences of 300 keys: 25 us, 38 in two parts).
+        per = std::max<int64_t>(
+            per, std::min<int64_t>(1024, (s.max_tokens * units + 1023) / 1024));
+        per = std::max<int64_t>(per, 2 * unit);
+    }
     p.chunk = (per + unit - 1) / unit * unit;
     p.splits = (s.max_tokens + p.chunk - 1) / p.chunk;
     p.logit_stride = s.weights ? (s.max_tokens + 63) / 64 * 64 : 0;   // whole steps

@@ -183,7 +183,7 @@ def attend(pool, table, lengths, q, counts=None, causal=True, scale=None):
     return out, w, mag, dots, big
 
 
-P_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -16, torch.float32: 2.0 ** -24}
+P_STEP = {torch.bfloat16: 2.0 ** -16, torch.float16: 2.0 ** -16, torch.float32: 2.0 ** -24}
 
 
 def weight_error(D, N, dots, big):
