@@ -9,20 +9,22 @@
 // kept tokens in ascending order.  All decisions are on integers, so nothing depends on
 // the order of the atomic increments.  Latency bounds it: a thread loads its keys (up to 16)
 // at once and keeps them in registers for all passes where the sequences fit one segment of
-// 1024 x 16 tokens; longer ones are read again, a segment at a time, in every pass.
+// 1024 x 16 tokens (256 of up to 16000 tokens: 18.7 us, 32 when every pass read them); longer
+// ones are read again, a segment at a time, in every pass.  One histogram is enough: 4, 8 or
+// 16 copies for neighbouring lanes took 21.8, 23.2 and 27.7 us where one took 21.7.
 //
 // evict_move_kernel, one workgroup per (sequence, key head, new block), keys and values
 // together (they share the lookups of indices and pages): gathers the block's kept rows,
 // takes their largest magnitude to the block's scale, and writes them rescaled by the ratio
-// of two powers of two.  It moves each kept byte once, and the copy rate bounds it.
+// of two powers of two.  It moves each kept byte once, and the copy rate bounds it: 280 MB
+// read and written, a row of 128 bytes here and there, take 47 to 56 us, 5.0 to 6.0 TB/s
+// (one block of keys or of values per workgroup: 63).
 #include "serve_device.h"
 #include "serve_kernels.h"
 
 namespace e2s {
 namespace {
 
-constexpr int kSelThreads = 1024;
-constexpr int kSelWaves = kSelThreads / kWave;
 constexpr int kBins = 2048;
 
 struct EvictArgs {
@@ -59,13 +61,15 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t ballot) {
                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(ballot), 0u));
 }
 
-template <int PER>                       // tokens per thread and segment
-__global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
+template <int THREADS, int PER>          // PER tokens per thread and segment
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictArgs a) {
+    constexpr int kSelWaves = THREADS / kWave;
+    constexpr int kOwn = kBins / THREADS;        // bins of a thread
     __shared__ uint32_t hist[kBins];
     __shared__ uint32_t sums[kSelWaves];
     __shared__ uint32_t ties[kSelWaves];
     __shared__ uint32_t found[3];             // digit, still wanted, of how many
-    constexpr int kSegment = kSelThreads * PER;
+    constexpr int kSegment = THREADS * PER;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int64_t b = blockIdx.x / a.G;
@@ -76,11 +80,11 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
     int32_t* keep = a.keep + (b * a.G + g) * static_cast<int64_t>(a.K);
     float* left = a.left ? a.left + b * a.ls[0] + g * a.ls[1] : nullptr;
     if (g == 0 && tid == 0) a.new_len[b] = kept;
-    for (int j = kept + tid; j < a.K; j += kSelThreads) keep[j] = -1;
+    for (int j = kept + tid; j < a.K; j += THREADS) keep[j] = -1;
     if (left)
-        for (int j = kept + tid; j < a.W; j += kSelThreads) left[j] = 0.0f;
+        for (int j = kept + tid; j < a.W; j += THREADS) left[j] = 0.0f;
     if (n <= a.K) {
-        for (int j = tid; j < n; j += kSelThreads) {
+        for (int j = tid; j < n; j += THREADS) {
             keep[j] = j;
             if (left) left[j] = w[j];
         }
@@ -115,8 +119,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
             const uint32_t mask = pass == 2 ? 1023u : 2047u;
-            hist[tid] = 0;
-            hist[tid + kSelThreads] = 0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) hist[tid + i * THREADS] = 0;
             __syncthreads();
             for (int seg = 0; seg < n; seg += kSegment) {
                 if (!once) load(seg);
@@ -127,24 +131,32 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
                 }
             }
             __syncthreads();
-            // thread t owns bins 2047 - 2t and 2046 - 2t: sums from the top
-            const uint32_t h1 = hist[kBins - 1 - 2 * tid], h0 = hist[kBins - 2 - 2 * tid];
-            uint32_t run = h1 + h0;
+            // thread t owns the kOwn bins below 2048 - kOwn t: sums from the top
+            uint32_t own[kOwn], all = 0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                own[i] = hist[kBins - 1 - kOwn * tid - i];
+                all += own[i];
+            }
+            uint32_t run = all;
             for (int o = 1; o < kWave; o <<= 1) {
                 const uint32_t v = __shfl_up(run, o);
                 if (lane >= o) run += v;
             }
             if (lane == kWave - 1) sums[wave] = run;
             __syncthreads();
-            uint32_t above = run - (h1 + h0);
+            uint32_t above = run - all;
 #pragma unroll
             for (int v = 0; v < kSelWaves; ++v) above += v < wave ? sums[v] : 0u;
             // the digit at which the count from the top reaches `want`
-            if (above < want && above + h1 + h0 >= want) {
-                const bool upper = above + h1 >= want;
-                found[0] = static_cast<uint32_t>(kBins - 1 - 2 * tid - (upper ? 0 : 1));
-                found[1] = want - above - (upper ? 0 : h1);
-                found[2] = upper ? h1 : h0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                if (above < want && above + own[i] >= want) {
+                    found[0] = static_cast<uint32_t>(kBins - 1 - kOwn * tid - i);
+                    found[1] = want - above;
+                    found[2] = own[i];
+                }
+                above += own[i];
             }
             __syncthreads();
             limit |= found[0] << shift;
@@ -353,12 +365,16 @@ hipError_t launch_cache_evict(const e2s_cache& c, const e2s_cache_evict_shape& s
     a.num_pages = c.num_pages;
     a.blocks = (s.budget + c.page_tokens - 1) / c.page_tokens;
     const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(s.batch) * a.G));
-    if (s.max_tokens <= kSelThreads)
-        hipLaunchKernelGGL(evict_select_kernel<1>, grid, dim3(kSelThreads), 0, st, a);
-    else if (s.max_tokens <= 4 * kSelThreads)
-        hipLaunchKernelGGL(evict_select_kernel<4>, grid, dim3(kSelThreads), 0, st, a);
+    // Small workgroups have short barriers and more of them fit a compute unit; all of a
+    // sequence's keys have to fit their registers.  640 tokens: 9.4 us for the call, 11.0 with
+    // 1024 threads; 64 sequences and 32 heads of 105 tokens 16 and 44, of 4000 tokens 122 with
+    // 512 threads, 119 with 256 x 16 keys and 153 with 1024; one of 4000 tokens 11.3, 12.9, 13.0.
+    if (s.max_tokens <= 1024)
+        hipLaunchKernelGGL((evict_select_kernel<256, 4>), grid, dim3(256), 0, st, a);
+    else if (s.max_tokens <= 4096)
+        hipLaunchKernelGGL((evict_select_kernel<512, 8>), grid, dim3(512), 0, st, a);
     else
-        hipLaunchKernelGGL(evict_select_kernel<16>, grid, dim3(kSelThreads), 0, st, a);
+        hipLaunchKernelGGL((evict_select_kernel<1024, 16>), grid, dim3(1024), 0, st, a);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     if (c.head_dim == 64) launch_move<64>(a, s.batch, st);

@@ -273,8 +273,10 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     int64_t per = p.shared_rows && p.tiles == 2 ? s.max_tokens
                                                 : (s.max_tokens * units + 2047) / 2048;
     // Short sequences: one workgroup of eight waves has all keys, and nothing is left to join.
-    // With few units that pays up to kFewKeys keys (one sequence, 4 key heads: 512 keys 7.8 us
-    // and 8.9 in parts, 1024 keys 10.4 and 9.4), with more of them up to kShortKeys (32 of 2000
+    // With few units that pays up to kFewKeys keys (one sequence, 4 key heads, on the device:
+    // 512 keys 7.8 us and 8.9 in parts, 1024 keys 10.4 and 9.4, 1536 keys 12.9 and 10.4; calls
+    // that the host makes one by one 9.5 and 10.5 at 1100 keys, since the join is a launch
+    // more), with more of them up to kShortKeys (32 of 2000
     // keys, 8 key heads: 25 us and 32; 64 of 1024: 24 and 31), until workgroups of four waves
     // fill the device unsplit (200 of 300 keys: 35 us and 25).
     p.waves = !p.shared_rows && units < 1024 &&

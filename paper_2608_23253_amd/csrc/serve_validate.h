@@ -42,7 +42,7 @@ struct AttendPlan {
 };
 constexpr int kAttendWaves = 4;
 constexpr int kAttendStep = 32;     // keys of a wave's step
-constexpr int64_t kFewKeys = 768, kShortKeys = 2048;
+constexpr int64_t kFewKeys = 1152, kShortKeys = 2048;
 AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s);
 
 }  // namespace e2s
