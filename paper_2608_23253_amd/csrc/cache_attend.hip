@@ -41,7 +41,8 @@
 // ahead from LDS, two waves a SIMD: 60).
 //
 // attend_finish_kernel joins the parts (21504 rows of up to 5: 6 us) and adds up few rows'
-// weights; attend_weights_kernel adds up weights where that is a launch of its own.
+// weights, attend_weights_kernel does where that is a launch of its own, and
+// attend_rows_weights_kernel adds up many rows'.
 #include <type_traits>
 
 #include "serve_device.h"
@@ -923,19 +924,6 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
                     if (kk >= min(limit[u], there[i >> 2])) y[i] = -kInf;
                 }
             }
-            if (a.logits) {
-                const int row = row0 + u * kTile + n16;
-                if (row < row_end) {
-                    float* to = a.logits +
-                                ((b * a.G + g) * static_cast<int64_t>(a.rows) + row) *
-                                    a.logit_stride + key + 4 * g4;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        *reinterpret_cast<f32x4*>(to + t * kTile) =
-                            f32x4{y[4 * t] * a.scale, y[4 * t + 1] * a.scale,
-                                  y[4 * t + 2] * a.scale, y[4 * t + 3] * a.scale};
-                }
-            }
             weigh<16, kDims>(y, a.scale, top[u], base[u], sum[u], o[u]);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -1201,7 +1189,7 @@ __global__ __launch_bounds__(kThreads) void attend_finish_kernel(const AttendArg
                   n0 + static_cast<int>(threadIdx.x) * 4, a.max_tokens);
 }
 
-// The tokens' weights from rows whose sums lie in the workspace.
+// The tokens' weights from few rows whose sums lie in the workspace.
 __global__ __launch_bounds__(kThreads) void attend_weights_kernel(const AttendArgs a,
                                                                   uint32_t blocks) {
     const uint32_t bg = blockIdx.x / blocks;
@@ -1210,6 +1198,127 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(const AttendAr
                     static_cast<int>(threadIdx.x)) * 4;
     token_weights(a, b, static_cast<int>(bg - b * a.G), a.lse + static_cast<int64_t>(bg) * a.rows,
                   attend_length(a, b), attend_count(a, b), n0, a.max_tokens);
+}
+
+// The tokens' weights from many rows, whose sums lie in the workspace: the logits are made a
+// second time, since through memory they would cost 8 bytes per row and key (16 sequences of
+// up to 48 queries and 4200 keys, 28 heads: 183 us for the call, 85 so, 55 without weights).
+// A wave holds the operands of its 64 keys and walks over the rows, 16 at a time (32 keys: 93
+// us, 16: 110); a lane adds up what its row of each tile gives 16 keys, and the 16 lanes of a
+// key are summed at the end.  Reading and widening the queries and the exponentials bound it.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void attend_rows_weights_kernel(const AttendArgs a,
+                                                                       uint32_t blocks) {
+    constexpr int kTerms = Terms<T>::n, kSteps = D / 32, kTiles = kWeightKeys / kTile;
+    const uint32_t bg = blockIdx.x / blocks;
+    const int64_t b = bg / static_cast<uint32_t>(a.G);
+    const int g = static_cast<int>(bg - static_cast<uint32_t>(b) * a.G);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, g4 = lane >> 4;
+    const int key0 =
+        (static_cast<int>(blockIdx.x % blocks) * kAttendWaves + wave) * kWeightKeys;
+    const int len = attend_length(a, b), count = attend_count(a, b);
+    if (key0 >= len) return;
+
+    const int64_t head = static_cast<int64_t>(g) * (D << a.page_shift);
+    bf16x8s kf[kTiles][kSteps];
+    bool there[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const int key = key0 + t * kTile;
+        int page = -1;
+        if (key < len) page = a.pages[b * a.pages_stride + (key >> a.page_shift)];
+        there[t] = page >= 0 && page < a.num_pages;
+        const int64_t pg = there[t] ? page : 0;
+        const float ks = there[t] ? a.k_scale[pg * a.G + g] : 1.0f;
+        const uint8_t* p = a.k + pg * a.k_page + head +
+                           ((key & ((1 << a.page_shift) - 1)) + n16) * D + g4 * 16;
+#pragma unroll
+        for (int h = 0; h < kSteps / 2; ++h) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(p + h * 64);
+            kf[t][2 * h] = widen8(w.x, w.y, ks);
+            kf[t][2 * h + 1] = widen8(w.z, w.w, ks);
+        }
+    }
+
+    // the first row that sees key0
+    const int rows = count * a.group;
+    const int first = a.causal ? max(0, key0 - len + count) * a.group / kTile * kTile : 0;
+    const float* lse = a.lse + static_cast<int64_t>(bg) * a.rows;
+    struct Tile {
+        Packet<T> q[kSteps];
+        float l;
+        int limit;
+    };
+    auto load = [&](int r0, Tile& x) {           // rows behind the last: it again, seeing nothing
+        const int row = min(r0 + n16, rows - 1), at = row / a.group;
+        x.limit = r0 + n16 < rows ? seen_by(a, len, count, at) : 0;
+        x.l = lse[row];
+        const T* src = static_cast<const T*>(a.q) + b * a.qs[0] +
+                       (g * a.group + row - at * a.group) * a.qs[1] + at * a.qs[2];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            x.q[s] = *reinterpret_cast<const Packet<T>*>(src + (s >> 1) * 64 + g4 * 16 +
+                                                         (s & 1) * 8);
+    };
+    float w[kTiles][4] = {};
+    if (first < rows) {
+        Tile next;
+        load(first, next);
+#pragma unroll 1
+        for (int r0 = first; r0 < rows; r0 += kTile) {
+            const Tile x = next;
+            load(r0 + kTile, next);
+            f32x4 s[kTiles];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < kSteps; ++e) {
+                bf16x8s qf[kTerms];
+                if constexpr (kTerms == 1) {
+                    qf[0] = __builtin_bit_cast(bf16x8s, x.q[e]);
+                } else {
+                    float f[8];
+                    unpack(x.q[e], f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        __bf16 part[kTerms];
+                        split_bf16<kTerms>(f[i], part);
+#pragma unroll
+                        for (int m = 0; m < kTerms; ++m) qf[m][i] = part[m];
+                    }
+                }
+#pragma unroll
+                for (int m = kTerms - 1; m >= 0; --m)
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][e], qf[m], s[t], 0,
+                                                                       0, 0);
+            }
+            const int limit = x.l == -kInf ? 0 : x.limit;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    w[t][r] += key0 + t * kTile + 4 * g4 + r < limit
+                                   ? exp2_hw(__builtin_fmaf(s[t][r], a.scale, -x.l))
+                                   : 0.0f;
+        }
+    }
+    const float* in = a.w_in ? a.w_in + b * a.wi[0] + g * a.wi[1] : nullptr;
+    float* out = a.w_out + b * a.wo[0] + g * a.wo[1];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float y = w[t][r];
+#pragma unroll
+            for (int o = 1; o < kTile; o <<= 1) y += __shfl_xor(y, o);
+            const int key = key0 + t * kTile + 4 * g4 + r;
+            if (!there[t]) y = 0.0f;
+            if (n16 == 0 && key < len) out[key] = in ? in[key] + y : y;
+        }
 }
 
 template <typename T, int D>
@@ -1254,7 +1363,13 @@ hipError_t launch_t(const AttendArgs& a, const AttendPlan& p, int64_t B, hipStre
         err = hipGetLastError();
         if (err != hipSuccess) return err;
     }
-    if (a.w_out && p.lse_kept) {
+    if (a.w_out && p.shared_rows) {
+        constexpr int kKeys = kWeightKeys * kAttendWaves;
+        const uint32_t per = static_cast<uint32_t>((a.max_tokens + kKeys - 1) / kKeys);
+        hipLaunchKernelGGL((attend_rows_weights_kernel<T, D>),
+                           dim3(static_cast<unsigned>(B * a.G) * per), block, 0, st, a, per);
+        err = hipGetLastError();
+    } else if (a.w_out && p.lse_kept) {
         hipLaunchKernelGGL(attend_weights_kernel,
                            dim3(static_cast<unsigned>(B * a.G) * blocks), block, 0, st, a, blocks);
         err = hipGetLastError();
@@ -1298,7 +1413,7 @@ hipError_t launch_cache_attend(const e2s_cache& c, const e2s_cache_attend_shape&
     }
     if (weights_out) {
         if (p.lse_kept) a.lse = reinterpret_cast<float*>(ws + p.lse_off);
-        a.logits = reinterpret_cast<float*>(ws + p.logit_off);
+        if (p.logit_stride > 0) a.logits = reinterpret_cast<float*>(ws + p.logit_off);
     }
     a.logit_stride = p.logit_stride;
     a.chunk = p.chunk;

@@ -210,7 +210,7 @@ e2s_status check_attend(const e2s_cache& c, const e2s_cache_attend_shape* s) {
     const double heads = static_cast<double>(s->batch) * c.num_kv_heads;
     // every kernel of the call: fewer than 2^32 work-items
     if (heads * p.row_groups * p.splits * 64 * p.waves >= 4294967296.0 ||
-        heads * (static_cast<double>(p.rows) + (s->max_tokens + 255) / 256) * 256.0 >= 4294967296.0)
+        heads * (static_cast<double>(p.rows) + (s->max_tokens + 127) / 128) * 256.0 >= 4294967296.0)
         return E2S_ERR_UNSUPPORTED;
     // and a workspace that 63 bits address
     if (heads * p.rows * (static_cast<double>(p.splits) * (c.head_dim + 2) + p.logit_stride) * 4.0 >
@@ -297,7 +297,8 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     }
     p.chunk = (per + unit - 1) / unit * unit;
     p.splits = (s.max_tokens + p.chunk - 1) / p.chunk;
-    p.logit_stride = s.weights ? (s.max_tokens + 63) / 64 * 64 : 0;   // whole steps
+    // Few rows keep their logits (in whole steps) for the tokens' weights; many make them twice.
+    p.logit_stride = s.weights && !p.shared_rows ? (s.max_tokens + 63) / 64 * 64 : 0;
     const size_t all = static_cast<size_t>(B * G * p.rows);
     size_t at = 0;
     auto region = [&](size_t floats) {

@@ -249,6 +249,30 @@ def test_attend(dtype, D, P, G, group, T, lengths):
     _check_attend(pool, table, lengths, q, order="token" if group % 2 else "head")
 
 
+@pytest.mark.parametrize("dtype,D,P,causal", [(BF, 128, 64, True), (HF, 64, 16, False),
+                                              (FL, 128, 32, True)])
+def test_attend_many_rows(dtype, D, P, causal):
+    """More than 32 rows to a key head, with ragged counts, missing pages and given weights:
+    the weights' own products."""
+    rng = np.random.default_rng(D + P)
+    lengths, counts = [700, 33, 12, 0, 260], [13, 0, 13, 4, 7]
+    pool, table = _filled(rng, lengths, 2, P, D)
+    table[0, 3], table[4, 0] = -1, 1 << 29
+    q = torch.from_numpy(rng.standard_normal((5, 10, 13, D)) * 2).to(dtype)
+    _check_attend(pool, table, lengths, q, counts=counts, causal=causal,
+                  weights_in=rng.random((5, 2, 700)).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", [BF, FL])
+def test_attend_some_rows_of_many_keys(dtype):
+    """17 to 32 rows where the keys are many enough that the rows are parted."""
+    rng = np.random.default_rng(23)
+    lengths = [33000, 700, 0, 32999]
+    pool, table = _filled(rng, lengths, 1, 128, 64)
+    q = torch.from_numpy(rng.standard_normal((4, 7, 3, 64))).to(dtype)
+    _check_attend(pool, table, lengths, q, max_tokens=33001, counts=[3, 1, 3, 2])
+
+
 def test_attend_many_splits():
     """A long sequence over many workgroups beside short ones; lengths above max_tokens are
     cut; added onto given weights."""

@@ -262,8 +262,8 @@ def test_attend_refusals():
 
 
 def test_attend_workspace():
-    """Nothing for a call of one part; with weights, the logits (and the rows' sums, where
-    the weights are a launch of their own)."""
+    """Nothing for a call of one part; with weights, few rows' logits (and the rows' sums,
+    where the weights are a launch of their own)."""
     def size(**kw):
         n = ctypes.c_size_t(0)
         c = desc()
@@ -277,7 +277,7 @@ def test_attend_workspace():
     assert size() == 0
     rows = 3 * 2 * 2 * 2                                 # B Hkv (H / Hkv) T
     assert size(weights=1) == up(rows * 128 * 4)
-    assert size(weights=1, num_queries=20) == up(10 * rows * 4) + up(10 * rows * 128 * 4)
+    assert size(weights=1, num_queries=20) == up(10 * rows * 4)
     assert size(max_tokens=100000) > 0
     c = desc()
     sh = attend_shape()
