@@ -631,7 +631,7 @@ __global__ __launch_bounds__(64 * WAVES, TILES == 1 ? 4 : 2) void attend_kernel(
                 for (int w = 1; w < WAVES; ++w) y[i] += lds.out[w][r][d0 + i];
             }
             const int64_t line = (b * a.G + g) * static_cast<int64_t>(a.rows) + row;
-            if (a.splits == 1) {
+            if (WAVES == 8 || a.splits == 1) {           // eight waves: never split
                 const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
                 const int t = row / a.group;
                 T* to = static_cast<T*>(a.out) + b * a.os[0] +
@@ -975,7 +975,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
         total += __shfl_xor(total, 32);
         if (row >= row_end) continue;
         const int64_t line = (b * a.G + g) * static_cast<int64_t>(a.rows) + row;
-        if (a.splits == 1) {
+        if (TILES == 2 || a.splits == 1) {           // 32 rows a wave: never split
             const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
             const int t = row / a.group;
             T* to = static_cast<T*>(a.out) + b * a.os[0] +

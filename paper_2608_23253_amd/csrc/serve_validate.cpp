@@ -267,7 +267,7 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     const int64_t units = B * G * p.row_groups;
     // Keys are split until 2048 workgroups fill the device, most of which have nothing to do
     // where sequences are of unequal lengths (16 of 300 to 4200 keys, up to 48 queries of 28
-    // heads: 60 us; 1536 workgroups: 74, 3072: 63).  Units of 32 rows to a wave are enough as
+    // heads: 60 us; 1536 workgroups: 74, 2560: 63).  Units of 32 rows to a wave are enough as
     // they are: 4 sequences of 512 queries and 2000 keys, 32 heads take 121 us unsplit, 169
     // and 178 in two and three parts.
     int64_t per = p.shared_rows && p.tiles == 2 ? s.max_tokens
