@@ -206,8 +206,12 @@ e2s_status check_attend(const e2s_cache& c, const e2s_cache_attend_shape* s) {
         E2S_TRY_(check_strides(s->weights_in_stride, wc, 2, s->max_tokens, 0, 0, 4));
         E2S_TRY_(check_strides(s->weights_out_stride, wc, 2, s->max_tokens, 1, 0, 4));
     }
-    const AttendPlan p = attend_plan(c, *s);
+    // Fewer than 2^24 rows in all (the join has a workgroup to a row), before the plan's
+    // products of rows and tokens, which 63 bits hold then.
     const double heads = static_cast<double>(s->batch) * c.num_kv_heads;
+    const double rows = static_cast<double>(s->num_heads / c.num_kv_heads) * s->num_queries;
+    if (heads * rows * 256.0 >= 4294967296.0) return E2S_ERR_UNSUPPORTED;
+    const AttendPlan p = attend_plan(c, *s);
     // every kernel of the call: fewer than 2^32 work-items
     if (heads * p.row_groups * p.splits * 64 * p.waves >= 4294967296.0 ||
         heads * (static_cast<double>(p.rows) + (s->max_tokens + 127) / 128) * 256.0 >= 4294967296.0)
