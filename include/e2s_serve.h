@@ -186,7 +186,8 @@ E2S_API e2s_status e2s_cache_attend_workspace_size(const e2s_cache* cache,
                                                    size_t* bytes);
 
 /* out = softmax(scale q . k) v over the cached tokens.
- *   q, out   [B, H, T, d]; base pointers and strides keep rows 16-byte aligned
+ *   q, out   [B, H, T, d]; base pointers and strides keep rows 16-byte aligned; out is
+ *            not q
  *   lengths  [B] int32: cached tokens, the queries' own among them (cut to 0 ..
  *            min(max_tokens, max_pages * P))
  *   q_count_opt [B] int32 or NULL (all T): sequence b's queries, cut to 0 .. T; rows of

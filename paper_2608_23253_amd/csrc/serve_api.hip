@@ -120,6 +120,8 @@ e2s_status e2s_cache_attend(const e2s_cache* cache, const e2s_cache_attend_shape
     const size_t bytes = e2s::attend_plan(*cache, *shape).bytes;
     if (bytes > 0) E2S_TRY(need(workspace, 256));
     if (workspace_bytes < bytes) return E2S_ERR_WORKSPACE_TOO_SMALL;
+    // many rows' weights read the queries again when the outputs are there
+    if (out == q) return E2S_ERR_BAD_PARAM;
     return from_hip(e2s::launch_cache_attend(*cache, *shape, pages, lengths, q_count_opt, q, out,
                                              weights_in_opt, weights_out_opt, workspace,
                                              static_cast<hipStream_t>(stream)));

@@ -1,0 +1,12 @@
+"""Calls of e2s_serve.h that are refused on the host because an output would overwrite what
+the call still reads, or another output (the fake device addresses are never dereferenced)."""
+import pytest
+
+from paper_2608_23253_amd import _lib as L
+from test_serve_abi import A, attend
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(weights=1, wout=4 * A), dict(num_queries=40),
+                                dict(num_queries=40, weights=1, wout=4 * A)])
+def test_attend_not_in_place(kw):
+    assert attend(q=2 * A, out=2 * A, **kw) == L.ERR_BAD_PARAM
