@@ -67,6 +67,10 @@ e2s_status e2s_rotate_positions(const e2s_rotary_shape* shape, const e2s_rotary_
         E2S_TRY(in_place(k, k_out, shape->k_stride, shape->k_out_stride,
                          {shape->batch, shape->k_heads, shape->num_tokens}));
     }
+    // each output is written while the other tensor's rows are still read, or written
+    if (shape->q_heads > 0 && shape->k_heads > 0 &&
+        (q_out == k_out || q_out == k || k_out == q))
+        return E2S_ERR_BAD_PARAM;
     return from_hip(e2s::launch_rotate(*shape, *plan, positions, q, k, q_out, k_out,
                                        static_cast<hipStream_t>(stream)));
 }
