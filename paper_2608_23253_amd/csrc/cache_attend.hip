@@ -212,7 +212,8 @@ __device__ __forceinline__ void token_weights(const AttendArgs& a, int64_t b, in
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    w[i] += n0 + i < limit ? exp2_hw(x[j][i] - l[j]) : 0.0f;
+                    // (-inf: no page, so no weight, also of a row whose sum is NaN)
+                    w[i] += n0 + i < limit && x[j][i] != -kInf ? exp2_hw(x[j][i] - l[j]) : 0.0f;
             }
         }
 #pragma unroll
