@@ -27,6 +27,11 @@ namespace {
 
 constexpr int kBins = 2048;
 
+// Maxima of held values are compared 2^-16 of their size: float32 has the largest, 2^128, and
+// the smallest, 2^-109, so (exact products of 4 bits and a power of two).
+constexpr int kDownBits = 16;
+constexpr float kDown = 1.0f / (1 << kDownBits);
+
 struct EvictArgs {
     const int32_t* pages;
     const int32_t* lengths;
@@ -273,7 +278,7 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(const EvictArgs a) 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(v[e]));   // skips NaN
             }
-            top = fmaxf(top, most * from[p][k]);
+            top = fmaxf(top, most * (from[p][k] * kDown));
         }
         top = wave_max(top);
         if ((threadIdx.x & (kWave - 1)) == 0) shared[k][threadIdx.x / kWave] = top;
@@ -284,7 +289,7 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(const EvictArgs a) 
         float top = shared[k][0];
 #pragma unroll
         for (int v = 1; v < THREADS / kWave; ++v) top = fmaxf(top, shared[k][v]);
-        to[k] = block_scale(top);
+        to[k] = block_scale<kDownBits>(top);
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {

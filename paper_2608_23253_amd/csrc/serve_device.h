@@ -30,10 +30,11 @@ template <> __device__ __forceinline__ float from_f32<float>(float x) { return x
 // ---------------------------------------------------------------------------
 constexpr int kLowestScale = -100;      // exponent of the smallest scale
 
-// The smallest 2^e, e >= kLowestScale, with amax <= 448 * 2^e.  amax = f * 2^x with f in
-// [1/2, 1), and 448 = 0.875 * 2^9.
+// The smallest 2^e, e >= kLowestScale, with amax * 2^SHIFT <= 448 * 2^e.  amax = f * 2^x with
+// f in [1/2, 1), and 448 = 0.875 * 2^9.
+template <int SHIFT = 0>
 __device__ __forceinline__ float block_scale(float amax) {
-    const int x = __builtin_amdgcn_frexp_expf(amax);
+    const int x = __builtin_amdgcn_frexp_expf(amax) + SHIFT;
     const float f = __builtin_amdgcn_frexp_mantf(amax);
     int e = f <= 0.875f ? x - 9 : x - 8;
     if (amax == 0.0f || e < kLowestScale) e = kLowestScale;

@@ -36,3 +36,36 @@ def test_nan_key_beside_a_missing_page(T, max_tokens):
     assert np.isnan(w[0, 0, :n][there]).all()
     assert (w[0, 0, :n][~there] == 0.25).all(), "a weight for tokens that no query sees"
     assert not np.isnan(w[1]).any() and (w[1, 0, :n][~there] == 0.25).all()
+
+
+def test_evict_moves_the_largest_values():
+    """Elements from 248 * 2^120 on are held as 2^128, which float32 does not have: moved to
+    another block they, and what shares the block, stay what they are."""
+    rng = np.random.default_rng(52)
+    D, P, G, n, K = 64, 16, 2, 40, 20
+    both, pages = S.tables(rng, [n, K], P, 1)
+    pool = S.Pool(pages, G, P, D)
+    rows = rng.standard_normal((G, n, D)) * 1e37
+    rows[0, 5], rows[1, 30, 3] = 3.35e38, -3.4e38
+    rows = rows.astype(np.float32).astype(np.float64)
+    for which in ("k", "v"):
+        pool.append(which, list(both[0]), 0, rows)
+    assert pool.ks[both[0][0], 0] == 2.0 ** 120 and pool.ks[both[0][1], 1] == 2.0 ** 120
+    cache = E.PagedCache.of(*pool.tensors())
+    w = np.zeros((1, G, n), np.float32)
+    w[0, :, 2:2 * K:2] = 1.0                          # tokens 2, 4 .. 38, and the first
+    w[0, 0, 5], w[0, 0, 4] = 1.0, 0.0
+    keep, _, _ = E.cache_evict(cache, _cuda(both[:1]), _ints([n]), _cuda(w), _cuda(both[1:]), K)
+    torch.cuda.synchronize()
+    for g in range(G):
+        idx = S.evict(w[0, g], n, K, 0, 0)
+        assert keep[0, g].tolist() == idx
+        for x, s in ((pool.k, pool.ks), (pool.v, pool.vs)):
+            for blk in range(-(-K // P)):
+                part = idx[blk * P:(blk + 1) * P]
+                held = np.stack([S._VALUES[x[both[0][i // P], g, i % P]]
+                                 * float(s[both[0][i // P], g]) for i in part])
+                sc = S.block_scale(np.abs(held).max())
+                x[both[1][blk], g, :len(part)] = S.to_e4m3(held / sc)
+                s[both[1][blk], g] = sc
+    _match(cache, pool)
