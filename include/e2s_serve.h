@@ -172,7 +172,7 @@ typedef struct {
     int32_t causal;         /* 1: the queries are the sequence's last tokens; 0: every
                                query sees all                                         */
     int32_t weights;        /* 1: weights_out is given; sizes the workspace           */
-    float scale;            /* logit scale, 0 .. 2e38; 0 selects 1/sqrt(d)            */
+    float scale;            /* logit scale, 0 .. 1e38; 0 selects 1/sqrt(d)            */
     int32_t reserved;       /* 0                                                      */
     int64_t pages_stride;
     int64_t q_stride[3];    /* sequence, head, query                                  */
@@ -200,7 +200,9 @@ E2S_API e2s_status e2s_cache_attend_workspace_size(const e2s_cache* cache,
  *            entries from len on are left as they were.  It may be weights_in itself,
  *            with its strides.
  * Logits, maxima, sums and the output accumulate in 32 bits; the weights that multiply
- * the values are rounded to 16 bits (bf16 and f16 q) or 24 bits (f32).
+ * the values are rounded to 16 bits (bf16 and f16 q) or 24 bits (f32).  The sums are divided
+ * by the weights' at the end: values below 2^116 cannot overflow on the way, and what adds
+ * less than 2^-110 may be lost.
  * workspace: 256-byte aligned, >= e2s_cache_attend_workspace_size bytes (NULL if 0),
  * contents undefined on return.  A NaN in a held key or value reaches the queries that
  * see it and no other. */

@@ -190,8 +190,8 @@ e2s_status check_attend(const e2s_cache& c, const e2s_cache_attend_shape* s) {
     if (!known_dtype(s->dtype) || s->reserved != 0) return E2S_ERR_BAD_PARAM;
     if ((s->causal != 0 && s->causal != 1) || (s->weights != 0 && s->weights != 1))
         return E2S_ERR_BAD_PARAM;
-    // (finite in log2 as well)
-    if (!(s->scale >= 0.0f && s->scale <= std::numeric_limits<float>::max() / 1.5f))
+    // (finite in log2 as well, and twice that)
+    if (!(s->scale >= 0.0f && s->scale <= std::numeric_limits<float>::max() / 3.0f))
         return E2S_ERR_BAD_PARAM;
     if (s->num_heads > kMaxHeads || s->max_tokens > kMaxCachedTokens ||
         s->num_queries > kMaxCachedTokens)

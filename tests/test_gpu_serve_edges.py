@@ -69,3 +69,44 @@ def test_evict_moves_the_largest_values():
                 x[both[1][blk], g, :len(part)] = S.to_e4m3(held / sc)
                 s[both[1][blk], g] = sc
     _match(cache, pool)
+
+
+@pytest.mark.parametrize("dtype", [BF, FL])
+@pytest.mark.parametrize("T,lengths,max_tokens", [
+    (1, [100, 7], 128), (1, [3000, 100], 3000), (1, [9000], 9000), (5, [300, 5], 2100),
+    (20, [2500, 300], 2500),
+])
+def test_attend_large_values(dtype, T, lengths, max_tokens):
+    """Values of one sign, of up to 2^127: their sum before the division by the weights' sum is
+    beyond float32, their mean is not."""
+    rng = np.random.default_rng(53)
+    pool, table = _filled(rng, lengths, 1, 64, 64)
+    pool.v &= 0x7F
+    pool.vs *= np.float32(2.0 ** 122)
+    q = torch.from_numpy(rng.standard_normal((len(lengths), 6, T, 64)) * 0.1).to(dtype)
+    _check_attend(pool, table, lengths, q, max_tokens=max_tokens)
+
+
+@pytest.mark.parametrize("T,max_tokens", [(1, 64), (1, 3000), (5, 2100), (20, 64)])
+def test_attend_the_largest_held_values(T, max_tokens):
+    """2^128, the largest that the cache holds, is no infinity: as a key's element where the
+    query's is 0, as a value of a token that gets no weight, and of one that gets some."""
+    rng = np.random.default_rng(54)
+    n, P, D = 40, 16, 64
+    pool, table = _filled(rng, [n], 1, P, D)
+    block, other = table[0, 0], table[0, 1]
+    pool.k[block, 0] = S.to_e4m3(np.zeros((P, D)))
+    pool.ks[block, 0] = 2.0 ** 120
+    pool.k[block, 0, 3, 7] = S.to_e4m3(np.array(256.0))              # 2^128
+    pool.v[other, 0] = S.to_e4m3(np.clip(rng.standard_normal((P, D)) * 50, -200, 200))
+    pool.vs[other, 0] = 2.0 ** 120
+    pool.v[other, 0, 2, 11] = S.to_e4m3(np.array(256.0))
+    pool.v[other, 0, 4] = S.to_e4m3(np.full(D, 256.0))
+    q = torch.from_numpy(rng.standard_normal((1, 6, T, D)) * 0.1).to(FL)
+    q[..., 7] = 0.0
+    # token 20 (row 4 of the second page) gets no weight: a key far on the other side
+    pool.k[other, 0, 4] = S.to_e4m3(np.zeros(D))
+    q[..., 9] = 30.0
+    pool.k[other, 0, 4, 9] = S.to_e4m3(np.array(-448.0))
+    pool.ks[other, 0] = 2.0 ** 4
+    _check_attend(pool, table, [n], q, max_tokens=max_tokens, causal=False)
