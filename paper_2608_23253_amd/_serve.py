@@ -199,6 +199,8 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
                              "with one B and T")
         if o is None:
             o = torch.empty_like(t)
+            if o.stride(3) != 1:     # rows one element apart: torch may order them first
+                o = torch.empty(shape, dtype=dtype, device=t.device)
             so = o.stride()
         else:
             so = _rows(o, name + "_out", dtype)

@@ -110,3 +110,16 @@ def test_attend_the_largest_held_values(T, max_tokens):
     pool.k[other, 0, 4, 9] = S.to_e4m3(np.array(-448.0))
     pool.ks[other, 0] = 2.0 ** 4
     _check_attend(pool, table, [n], q, max_tokens=max_tokens, causal=False)
+
+
+def test_rotate_rows_that_overlap():
+    """Rows one element apart (windows over one line): the output's rows do not overlap."""
+    D, T, H = 64, 5, 3
+    line = torch.randn(4000, generator=torch.Generator().manual_seed(5)).cuda()
+    q = line.as_strided((2, H, T, D), (1000, 300, 1, 1))
+    k = line.as_strided((2, T, H, D), (0, 0, 1, 1)).transpose(1, 2)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") * 7
+    plan = E.rotary_plan(D)
+    got = E.rotate_positions(q, k, pos, plan)
+    want = E.rotate_positions(q.contiguous(), k.contiguous(), pos, plan)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
