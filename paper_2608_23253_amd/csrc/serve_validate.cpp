@@ -16,15 +16,15 @@ bool known_dtype(int32_t t) {
 }
 
 // Strides of an input (`least` 0) or of an output (1, asked only where the count is above
-// one): within range, whole 16-byte rows where `align` is given (elements per 16 bytes),
-// and the last row's end addressable.
+// one): within range, whole 16-byte rows where `align` is given (elements per 16 bytes; a
+// stride that only index 0 takes may be anything), and the last row's end addressable.
 e2s_status check_strides(const int64_t* st, const int64_t* counts, int n, int64_t row, int least,
                          int64_t align, int bytes) {
     double end = static_cast<double>(row);
     for (int i = 0; i < n; ++i) {
         if (st[i] < 0 || st[i] > kMaxStride) return E2S_ERR_BAD_SHAPE;
         if (counts[i] > 1 && st[i] < least) return E2S_ERR_BAD_SHAPE;
-        if (align > 0 && st[i] % align != 0) return E2S_ERR_MISALIGNED;
+        if (align > 0 && counts[i] > 1 && st[i] % align != 0) return E2S_ERR_MISALIGNED;
         if (counts[i] > 1)
             end += static_cast<double>(counts[i] - 1) * static_cast<double>(st[i]);
     }
