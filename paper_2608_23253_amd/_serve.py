@@ -317,7 +317,8 @@ def cache_append(cache: PagedCache, pages, start, k, v, count=None, src_idx=None
 class CacheAttention:
     """Repeated e2s_cache_attend calls of one shape: `batch` sequences of at most
     `max_tokens` cached tokens and `num_queries` queries.  It holds the workspace, so calls
-    of one object on several streams are the caller's to order."""
+    of one object on several streams are the caller's to order, and a stream that a call
+    was given has to be there until the object is dropped."""
 
     def __init__(self, cache: PagedCache, batch: int, num_heads: int, num_queries: int,
                  max_tokens: int, dtype=None, scale: float = 0.0, causal: bool = True,
@@ -340,6 +341,13 @@ class CacheAttention:
         _raise(_LIB.e2s_cache_attend_workspace_size(cache.desc_ref, sh, ctypes.byref(n)),
                "e2s_cache_attend_workspace_size")
         self.workspace = torch.empty(int(n.value), device=cache.device, dtype=torch.uint8)
+        # streams whose work the allocator waits for before it gives the workspace away
+        self._streams = {_lib._CURRENT_STREAM(cache.device.index)}
+
+    def _used_on(self, stream: int):
+        torch = _torch()
+        self.workspace.record_stream(torch.cuda.ExternalStream(stream, device=self.cache.device))
+        self._streams.add(stream)
 
     def _weights(self, t, name):
         torch = _torch()
@@ -382,6 +390,9 @@ class CacheAttention:
                 wi = self._weights(weights_in, "weights_in")
         elif weights_in is not None or weights_out is not None:
             raise ValueError("this CacheAttention was made without weights")
+        at = _lib._CURRENT_STREAM(self.cache.device.index) if stream is None else stream
+        if at not in self._streams:
+            self._used_on(at)
         sh = _ATTEND.pack(*self._head, width, *self._tail, row, *qs[:3], *os_[:3], *wi, *wo)
         _launch("e2s_cache_attend",
                 (self.workspace, q, pages, lengths, out, q_count, weights_in, weights_out),

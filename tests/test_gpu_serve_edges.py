@@ -123,3 +123,32 @@ def test_rotate_rows_that_overlap():
     got = E.rotate_positions(q, k, pos, plan)
     want = E.rotate_positions(q.contiguous(), k.contiguous(), pos, plan)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_workspace_outlives_the_object_on_another_stream(given):
+    """An object that is dropped while another stream still works in its workspace: the
+    allocator keeps the memory until that work is done."""
+    rng = np.random.default_rng(55)
+    pool, table = _filled(rng, [5000], 2, 64, 128)
+    q = torch.from_numpy(rng.standard_normal((1, 4, 1, 128))).to(BF).cuda()
+    cache, pages, lengths = E.PagedCache.of(*pool.tensors()), _cuda(table), _ints([5000])
+    want, _ = E.cache_attend(q, cache, pages, lengths)
+    torch.cuda.synchronize()
+    att = E.CacheAttention(cache, 1, 4, 1, 5000)
+    size, at = att.workspace.numel(), att.workspace.data_ptr()
+    assert size > 0
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    if given:
+        got, _ = att(q, pages, lengths, stream=side.cuda_stream)
+    else:
+        with torch.cuda.stream(side):
+            got, _ = att(q, pages, lengths)
+    assert not side.query(), "the other stream's work was to be under way still"
+    del att
+    new = torch.empty(size, dtype=torch.uint8, device="cuda")
+    assert new.data_ptr() != at
+    side.synchronize()
+    assert torch.equal(got, want)
