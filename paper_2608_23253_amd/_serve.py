@@ -125,6 +125,17 @@ def _rows(t, name, dtype=None):
     return st
 
 
+def _rows_like(t):
+    """An empty output for rows as t's, and its strides."""
+    torch = _torch()
+    o = torch.empty_like(t)
+    st = o.stride()
+    if st[3] != 1:                       # rows one element apart: torch may order them first
+        o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        st = o.stride()
+    return o, st
+
+
 def _vector(t, name, n):
     """The address of an int32 [n] of per-sequence numbers."""
     torch = _torch()
@@ -171,7 +182,7 @@ def rotary_plan(head_dim: int, rot_dim: Optional[int] = None, base: float = 1000
 
 
 def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q_out=None,
-                     k_out=None):
+                     k_out=None, stream: Optional[int] = None):
     """q [B, H, T, d] and k [B, Hkv, T, d] (either may be None; any strides with contiguous
     rows) turned by `positions`: int32 [T] or [B, T], with a leading 3 for a plan of three
     axes.  inverse turns back: the transpose, which takes a gradient of the outputs to that
@@ -198,10 +209,11 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
             raise ValueError(f"{name} {tuple(shape)} must be [B, heads, T, {D}] "
                              "with one B and T")
         if o is None:
-            o = torch.empty_like(t)
-            if o.stride(3) != 1:     # rows one element apart: torch may order them first
-                o = torch.empty(shape, dtype=dtype, device=t.device)
-            so = o.stride()
+            if stream is None:
+                o, so = _rows_like(t)
+            else:
+                with _allocating_on(stream, t.device):
+                    o, so = _rows_like(t)
         else:
             so = _rows(o, name + "_out", dtype)
             if o.shape != shape:
@@ -229,7 +241,8 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
         sh = _ROTARY.pack(B, T, *heads, _dtype_code(x), 1 if inverse else 0, *strides,
                           *out_strides, *ps)
         _launch("e2s_rotate_positions", (q, k, positions, *outs), _LIB.e2s_rotate_positions, sh,
-                ctypes.byref(plan), positions.data_ptr(), ptrs[0], ptrs[2], ptrs[1], ptrs[3])
+                ctypes.byref(plan), positions.data_ptr(), ptrs[0], ptrs[2], ptrs[1], ptrs[3],
+                stream=stream)
     return outs[0], outs[1]
 
 
@@ -404,7 +417,8 @@ class CacheAttention:
 
 def cache_attend(q, cache: PagedCache, pages, lengths, max_tokens: Optional[int] = None,
                  scale: float = 0.0, causal: bool = True, out=None, q_count=None,
-                 want_weights: bool = False, weights_in=None, weights_out=None):
+                 want_weights: bool = False, weights_in=None, weights_out=None,
+                 stream: Optional[int] = None):
     """One CacheAttention call: (out, weights or None).  max_tokens: no length is larger
     (default: what the page table can hold)."""
     _rows(q, "q")
@@ -412,9 +426,10 @@ def cache_attend(q, cache: PagedCache, pages, lengths, max_tokens: Optional[int]
     if max_tokens is None:
         max_tokens = pages.shape[1] * cache.page_tokens
     weights = want_weights or weights_in is not None or weights_out is not None
-    call = CacheAttention(cache, q.shape[0], q.shape[1], q.shape[2], max_tokens, q.dtype, scale,
-                          causal, weights)
-    return call(q, pages, lengths, out, q_count, weights_in, weights_out)
+    with _allocating_on(stream, q.device):
+        call = CacheAttention(cache, q.shape[0], q.shape[1], q.shape[2], max_tokens, q.dtype,
+                              scale, causal, weights)
+    return call(q, pages, lengths, out, q_count, weights_in, weights_out, stream)
 
 
 def cache_evict(cache: PagedCache, pages, lengths, weights, new_pages, budget: int,

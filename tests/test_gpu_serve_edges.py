@@ -152,3 +152,29 @@ def test_workspace_outlives_the_object_on_another_stream(given):
     assert new.data_ptr() != at
     side.synchronize()
     assert torch.equal(got, want)
+
+
+def test_rotate_and_attend_on_a_given_stream():
+    """`stream` without entering it, for every call: their work waits for what is on that
+    stream, and the current one stays free."""
+    rng = np.random.default_rng(56)
+    pool, table = _filled(rng, [300, 5000], 2, 64, 64)
+    cache, pages, lengths = E.PagedCache.of(*pool.tensors()), _cuda(table), _ints([300, 5000])
+    q = torch.from_numpy(rng.standard_normal((2, 4, 2, 64))).to(BF).cuda()
+    pos = torch.arange(2, dtype=torch.int32, device="cuda")
+    plan = E.rotary_plan(64)
+    turned, _ = E.rotate_positions(q, None, pos, plan)
+    out, w = E.cache_attend(turned, cache, pages, lengths, want_weights=True)
+    src = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        src.copy_(q)
+    a, _ = E.rotate_positions(src, None, pos, plan, stream=side.cuda_stream)
+    b, w2 = E.cache_attend(a, cache, pages, lengths, want_weights=True, stream=side.cuda_stream)
+    torch.cuda.current_stream().synchronize()
+    assert not side.query(), "the calls were to wait for the other stream's work"
+    side.synchronize()
+    for x, y in ((turned, a), (out, b), (w, w2)):
+        assert torch.equal(x, y)
