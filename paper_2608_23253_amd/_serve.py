@@ -103,6 +103,10 @@ _ATTEND = struct.Struct("@8ifi11q")
 _EVICT = struct.Struct("@8i6q")
 
 
+# (the binding loads without torch, too)
+_Function = _lib._TORCH.autograd.Function if _lib._TORCH is not None else object
+
+
 def _allocating_on(stream, device):
     """What a call allocates, and fills with zeros, belongs to the stream it runs on."""
     if stream is None:
@@ -181,16 +185,44 @@ def rotary_plan(head_dim: int, rot_dim: Optional[int] = None, base: float = 1000
     return plan
 
 
+class _Rotate(_Function):
+    """The rotation, whose transpose is the rotation back."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, plan, inverse):
+        ctx.save_for_backward(positions)
+        ctx.plan, ctx.inverse = plan, inverse
+        ctx.set_materialize_grads(False)
+        return rotate_positions(q, k, positions, plan, inverse)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        # (a broadcast gradient has no contiguous rows)
+        gq, gk = (g.contiguous() if need and g is not None and g.stride(3) != 1 else
+                  g if need else None for g, need in zip(grads, ctx.needs_input_grad))
+        if gq is None and gk is None:
+            return None, None, None, None, None
+        return (*rotate_positions(gq, gk, *ctx.saved_tensors, ctx.plan, not ctx.inverse), None,
+                None, None)
+
+
 def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q_out=None,
                      k_out=None, stream: Optional[int] = None):
     """q [B, H, T, d] and k [B, Hkv, T, d] (either may be None; any strides with contiguous
     rows) turned by `positions`: int32 [T] or [B, T], with a leading 3 for a plan of three
     axes.  inverse turns back: the transpose, which takes a gradient of the outputs to that
-    of the inputs.  Returns (q_out, k_out); an output may be its input."""
+    of the inputs.  Returns (q_out, k_out); an output may be its input.  Outputs that are
+    not given have a gradient where the inputs ask for one."""
     torch = _torch()
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
+    if torch.is_grad_enabled() and (x.requires_grad or (k is not None and k.requires_grad)):
+        if q_out is not None or k_out is not None:
+            raise ValueError("an output that is given has no gradient: give none, or call "
+                             "under torch.no_grad()")
+        with _allocating_on(stream, x.device):
+            return _Rotate.apply(q, k, positions, plan, inverse)
     dtype, B, T, D = x.dtype, x.shape[0], x.shape[2], plan.head_dim
     heads, strides, out_strides, ptrs, outs = [], [], [], [], []
     for t, name, o in ((q, "q", q_out), (k, "k", k_out)):

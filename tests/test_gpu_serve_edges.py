@@ -178,3 +178,94 @@ def test_rotate_and_attend_on_a_given_stream():
     side.synchronize()
     for x, y in ((turned, a), (out, b), (w, w2)):
         assert torch.equal(x, y)
+
+
+def _grad_of_formula(x, w, pos, f, kw):
+    y = x.double().requires_grad_()
+    S.rotate(y, pos, f, layout=kw["layout"], inverse=kw["inverse"]).backward(w.double())
+    return y.grad
+
+
+@pytest.mark.parametrize("dtype", [BF, FL])
+@pytest.mark.parametrize("layout,inverse", [("half", False), ("interleaved", True)])
+def test_rotation_has_its_gradient(dtype, layout, inverse):
+    g = torch.Generator().manual_seed(6)
+    R, D = 32, 64
+    x, w = (torch.randn((2, 3, 9, D), generator=g).to(dtype) for _ in range(2))
+    k, wk = (torch.randn((2, 1, 9, D), generator=g).to(dtype) for _ in range(2))
+    pos = torch.randint(0, 500, (2, 9), generator=g, dtype=torch.int32)
+    plan, f = E.rotary_plan(D, rot_dim=R, layout=layout), S.frequencies(R, 1e4)
+    kw = dict(layout=layout, inverse=inverse)
+    q1, k1 = x.cuda().requires_grad_(), k.cuda().requires_grad_()
+    yq, yk = E.rotate_positions(q1, k1, pos.cuda(), plan, inverse=inverse)
+    with torch.no_grad():
+        plain = E.rotate_positions(q1, k1, pos.cuda(), plan, inverse=inverse)
+    assert torch.equal(yq, plain[0]) and torch.equal(yk, plain[1])
+    assert not plain[0].requires_grad
+    torch.autograd.backward([yq, yk], [w.cuda(), wk.cuda()])
+    for got, a, b in ((q1.grad, x, w), (k1.grad, k, wk)):
+        ref = _grad_of_formula(a, b, pos, f, kw)
+        tol = S.rotate_tolerance(b.double(), ref, R, layout, dtype)
+        assert ((got.cpu().double() - ref).abs() <= tol).all()
+    # one of the two alone, through a loss whose gradient is one broadcast number
+    q2 = x.cuda().requires_grad_()
+    yq, yk = E.rotate_positions(q2, k.cuda(), pos.cuda(), plan, inverse=inverse)
+    yq.sum().backward()
+    ones = torch.ones_like(x)
+    ref = _grad_of_formula(x, ones, pos, f, kw)
+    tol = S.rotate_tolerance(ones.double(), ref, R, layout, dtype)
+    assert ((q2.grad.cpu().double() - ref).abs() <= tol).all()
+    # against differences: the map is linear, so a step of 1 is exact but for the roundings of
+    # its two results (a half step of the type and 8 * 2^-24 of |x0| + |x1| each)
+    for at in ((0, 1, 3, 5), (1, 2, 8, 30), (1, 0, 0, 50)):
+        up, down = x.double(), x.double()
+        up[at] += 1
+        down[at] -= 1
+        up, down = up.to(dtype), down.to(dtype)
+        step = float(up[at].double() - down[at].double())
+        with torch.no_grad():
+            y1, _ = E.rotate_positions(up.cuda(), None, pos.cuda(), plan, inverse=inverse)
+            y0, _ = E.rotate_positions(down.cuda(), None, pos.cuda(), plan, inverse=inverse)
+        slope = float(((y1.double() - y0.double()).cpu() * w.double())[at[:3]].sum()) / step
+        # only the element's own row changes, and of it the pair
+        row = at[:3]
+        big = 2 * (up[row].abs().max() + 1).double()
+        tol = 2 * 2 * (S.HALF_STEP[dtype] + 8 * 2.0 ** -24) * float(big * w[row].double().abs().max())
+        assert abs(slope - float(q1.grad[at])) <= tol / step + \
+            S.HALF_STEP[dtype] * abs(slope) + 1e-6
+
+
+def test_rotation_gradients_of_shared_and_strided_inputs():
+    """A query that all heads share, token-major rows, a second derivative, and no gradient
+    where none is asked for."""
+    g = torch.Generator().manual_seed(7)
+    D, T, H = 64, 11, 4
+    one = torch.randn((2, 1, T, D), generator=g).cuda().requires_grad_()
+    wide = torch.randn((2, T, H, D), generator=g).cuda().requires_grad_()
+    w = torch.randn((2, H, T, D), generator=g).cuda()
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") * 31
+    plan = E.rotary_plan(D)
+    yq, yk = E.rotate_positions(one.expand(2, H, T, D), wide.transpose(1, 2), pos, plan)
+    assert yq.requires_grad and yk.requires_grad
+    gq, gk = torch.autograd.grad([yq, yk], [one, wide], [w, w], create_graph=True)
+    with torch.no_grad():
+        back, _ = E.rotate_positions(w, None, pos, plan, inverse=True)
+    assert torch.equal(gk, back.transpose(1, 2))
+    # (four heads summed in float32)
+    assert ((gq - back.sum(1, keepdim=True)).abs()
+            <= 8 * 2.0 ** -24 * back.abs().sum(1, keepdim=True)).all()
+    # the gradient is linear in w: its own derivative is the rotation
+    w2 = w.clone().requires_grad_()
+    y, _ = E.rotate_positions(wide.transpose(1, 2), None, pos, plan)
+    gx, = torch.autograd.grad(y, wide, w2, create_graph=True)
+    v = torch.randn((2, T, H, D), generator=g).cuda()
+    gw, = torch.autograd.grad(gx, w2, v)
+    with torch.no_grad():
+        there, _ = E.rotate_positions(v.transpose(1, 2), None, pos, plan)
+    assert torch.equal(gw, there)
+    with pytest.raises(ValueError):
+        E.rotate_positions(wide.transpose(1, 2), None, pos, plan, q_out=torch.empty_like(w))
+    out = torch.empty_like(w)
+    with torch.no_grad():
+        E.rotate_positions(wide.transpose(1, 2), None, pos, plan, q_out=out)
+    assert torch.equal(out, y)
