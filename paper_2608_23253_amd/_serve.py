@@ -359,6 +359,20 @@ def cache_append(cache: PagedCache, pages, start, k, v, count=None, src_idx=None
             _ptr(src_idx), k.data_ptr(), v.data_ptr(), stream=stream)
 
 
+class _Undifferentiated(_Function):
+    """The outputs of call(), whose gradient is asked for in vain: an error says so where it
+    would otherwise be lost."""
+
+    @staticmethod
+    def forward(ctx, q, call):
+        return call()
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("attention over the 8-bit cache has no backward pass: call it under "
+                           "torch.no_grad() or with detached queries")
+
+
 class CacheAttention:
     """Repeated e2s_cache_attend calls of one shape: `batch` sequences of at most
     `max_tokens` cached tokens and `num_queries` queries.  It holds the workspace, so calls
@@ -408,9 +422,20 @@ class CacheAttention:
                  weights_out=None, stream: Optional[int] = None):
         """q [B, H, T, d] against each sequence's lengths[b] cached tokens: (out, weights_out
         or None).  See e2s_cache_attend for q_count, weights_in and weights_out; outputs not
-        given are allocated, zeros where the call leaves entries as they were."""
+        given are allocated, zeros where the call leaves entries as they were.  There is no
+        backward pass: where q asks for a gradient, `out` is not given and a backward pass
+        through the outputs is an error."""
         torch = _torch()
         qs = _rows(q, "q", self.dtype)
+        if torch.is_grad_enabled() and q.requires_grad:
+            if out is not None:
+                raise ValueError("attention over the cache has no gradient for `out`: call it "
+                                 "under torch.no_grad() or with detached queries")
+            if self.weights and weights_out is None:
+                return _Undifferentiated.apply(q, lambda: self(
+                    q, pages, lengths, None, q_count, weights_in, None, stream))
+            return _Undifferentiated.apply(q, lambda: self(
+                q, pages, lengths, None, q_count, weights_in, weights_out, stream)[0]), weights_out
         if q.shape != self._q_shape:
             raise ValueError(f"q must be {list(self._q_shape)} (got {list(q.shape)})")
         width, row = _table(pages, "pages", self.batch)

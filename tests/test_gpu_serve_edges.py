@@ -269,3 +269,28 @@ def test_rotation_gradients_of_shared_and_strided_inputs():
     with torch.no_grad():
         E.rotate_positions(wide.transpose(1, 2), None, pos, plan, q_out=out)
     assert torch.equal(out, y)
+
+
+def test_attention_says_that_it_has_no_gradient():
+    rng = np.random.default_rng(57)
+    pool, table = _filled(rng, [100], 2, 16, 64)
+    cache, pages, lengths = E.PagedCache.of(*pool.tensors()), _cuda(table), _ints([100])
+    q = torch.from_numpy(rng.standard_normal((1, 4, 2, 64))).to(BF).cuda()
+    want, ww = E.cache_attend(q, cache, pages, lengths, want_weights=True)
+    q.requires_grad_()
+    out, w = E.cache_attend(q, cache, pages, lengths, want_weights=True)
+    assert torch.equal(out, want) and torch.equal(w, ww)
+    for y in (out, w):
+        with pytest.raises(RuntimeError, match="no backward"):
+            y.float().sum().backward(retain_graph=True)
+    acc = torch.zeros_like(ww)
+    out, w = E.cache_attend(q, cache, pages, lengths, weights_in=acc, weights_out=acc)
+    assert w is acc and torch.equal(acc, ww)
+    with pytest.raises(RuntimeError, match="no backward"):
+        out.float().sum().backward()
+    with pytest.raises(ValueError):
+        E.cache_attend(q, cache, pages, lengths, out=torch.empty_like(want))
+    with torch.no_grad():
+        given = torch.empty_like(want)
+        out, _ = E.cache_attend(q, cache, pages, lengths, out=given)
+    assert out is given and torch.equal(out, want) and not out.requires_grad
