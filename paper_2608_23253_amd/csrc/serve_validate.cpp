@@ -277,10 +277,12 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     int64_t per = p.shared_rows && p.tiles == 2 ? s.max_tokens
                                                 : (s.max_tokens * units + 2047) / 2048;
     // Short sequences: one workgroup of eight waves has all keys, and nothing is left to join.
-    // With few units that pays up to kFewKeys keys (one sequence, 4 key heads, on the device:
-    // 512 keys 7.8 us and 8.9 in parts, 1024 keys 10.4 and 9.4, 1536 keys 12.9 and 10.4; calls
-    // that the host makes one by one 9.5 and 10.5 at 1100 keys, since the join is a launch
-    // more), with more of them up to kShortKeys (32 of 2000
+    // With few units that pays up to kFewKeys keys.  Captured calls of 4 units, 28 heads at
+    // d = 128, take 8.6 us and 8.9 in parts with 768 keys, 9.7 and 9.3 with 1024, 10.8 and 9.8
+    // with 1152 (f32 9.7 and 9.5, 11.4 and 10.0, 12.9 and 10.4); of 120 units 10.7 and 12.1 with
+    // 1024, 13.0 and 14.3 with 1280; at d = 64 7.9 and 8.4 with 1024, 9.9 and 9.2 with 1536.
+    // Calls that the host makes one by one pay for the join's launch: 9.6 and 11.3 with 1024,
+    // 12.0 and 11.2 with 1536.  With more units it pays up to kShortKeys (32 of 2000
     // keys, 8 key heads: 25 us and 32; 64 of 1024: 24 and 31), until workgroups of four waves
     // fill the device unsplit (200 of 300 keys: 35 us and 25).
     p.waves = !p.shared_rows && units < 1024 &&

@@ -43,7 +43,7 @@ struct AttendPlan {
 constexpr int kAttendWaves = 4;
 constexpr int kAttendStep = 32;     // keys of a wave's step
 constexpr int kWeightKeys = 64;     // keys of a wave that adds up many rows' weights
-constexpr int64_t kFewKeys = 1152, kShortKeys = 2048;
+constexpr int64_t kFewKeys = 1024, kShortKeys = 2048;
 AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s);
 
 }  // namespace e2s

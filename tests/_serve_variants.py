@@ -81,6 +81,14 @@ CALLS = {
         dtype="bf16", batch=40, heads=32, kv_heads=8, queries=1, head_dim=128, page=64,
         max_tokens=2000, lengths=[2000, 256, 0, 1], rest=90, weights=True,
         plan=dict(shared_rows=0, tiles=1, waves=8, splits=1, lse_kept=0)),
+    "eight_waves_one_sequence": dict(
+        dtype="bf16", batch=1, heads=8, kv_heads=2, queries=1, head_dim=128, page=64,
+        max_tokens=1024, lengths=[1024], weights=True,
+        plan=dict(shared_rows=0, tiles=1, waves=8, splits=1)),
+    "parts_of_one_sequence": dict(
+        dtype="bf16", batch=1, heads=8, kv_heads=2, queries=1, head_dim=128, page=64,
+        max_tokens=1025, lengths=[1025], weights=True,
+        plan=dict(shared_rows=0, tiles=1, waves=4, few_parts=1)),
     "eight_waves_two_tiles_bf16_128": dict(
         dtype="bf16", batch=2, heads=14, kv_heads=2, queries=4, head_dim=128, page=32,
         max_tokens=700, lengths=[700, 3], weights=True,
