@@ -16,7 +16,7 @@ import struct
 from typing import Optional
 
 from . import _lib
-from ._lib import _check, _dtype_code, _launch, _ptr, _raise, _torch
+from ._lib import _CURRENT_STREAM, _check, _dtype_code, _launch, _ptr, _raise, _torch
 
 HEADER = os.path.join(os.path.dirname(_lib.PKG), "include", "e2s_serve.h")
 
@@ -118,6 +118,12 @@ def _allocating_on(stream, device):
 _HERE = contextlib.nullcontext()
 
 
+def _like(t, stream, order=None):
+    torch = _torch()
+    with _allocating_on(stream, t.device):
+        return torch.empty_like(t, memory_format=order or torch.preserve_format)
+
+
 def _rows(t, name, dtype=None):
     """The strides of a [B, H, T, d] tensor of rows: any, the last dimension contiguous."""
     if not (isinstance(t, _torch().Tensor) and t.is_cuda and t.dim() == 4 and
@@ -127,17 +133,6 @@ def _rows(t, name, dtype=None):
     if st[3] != 1 and t.shape[3] > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
     return st
-
-
-def _rows_like(t):
-    """An empty output for rows as t's, and its strides."""
-    torch = _torch()
-    o = torch.empty_like(t)
-    st = o.stride()
-    if st[3] != 1:                       # rows one element apart: torch may order them first
-        o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        st = o.stride()
-    return o, st
 
 
 def _vector(t, name, n):
@@ -217,7 +212,7 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
-    if torch.is_grad_enabled() and (x.requires_grad or (k is not None and k.requires_grad)):
+    if (x.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
         if q_out is not None or k_out is not None:
             raise ValueError("an output that is given has no gradient: give none, or call "
                              "under torch.no_grad()")
@@ -241,11 +236,11 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
             raise ValueError(f"{name} {tuple(shape)} must be [B, heads, T, {D}] "
                              "with one B and T")
         if o is None:
-            if stream is None:
-                o, so = _rows_like(t)
-            else:
-                with _allocating_on(stream, t.device):
-                    o, so = _rows_like(t)
+            o = _like(t, stream) if stream is not None else torch.empty_like(t)
+            so = o.stride()
+            if so[3] != 1:               # rows one element apart: torch may order them first
+                o = _like(t, stream, torch.contiguous_format)
+                so = o.stride()
         else:
             so = _rows(o, name + "_out", dtype)
             if o.shape != shape:
@@ -401,7 +396,8 @@ class CacheAttention:
                "e2s_cache_attend_workspace_size")
         self.workspace = torch.empty(int(n.value), device=cache.device, dtype=torch.uint8)
         # streams whose work the allocator waits for before it gives the workspace away
-        self._streams = {_lib._CURRENT_STREAM(cache.device.index)}
+        self._index = cache.device.index
+        self._streams = {_CURRENT_STREAM(self._index)}
 
     def _used_on(self, stream: int):
         torch = _torch()
@@ -427,7 +423,7 @@ class CacheAttention:
         through the outputs is an error."""
         torch = _torch()
         qs = _rows(q, "q", self.dtype)
-        if torch.is_grad_enabled() and q.requires_grad:
+        if q.requires_grad and torch.is_grad_enabled():
             if out is not None:
                 raise ValueError("attention over the cache has no gradient for `out`: call it "
                                  "under torch.no_grad() or with detached queries")
@@ -460,9 +456,10 @@ class CacheAttention:
                 wi = self._weights(weights_in, "weights_in")
         elif weights_in is not None or weights_out is not None:
             raise ValueError("this CacheAttention was made without weights")
-        at = _lib._CURRENT_STREAM(self.cache.device.index) if stream is None else stream
-        if at not in self._streams:
-            self._used_on(at)
+        if stream is None:
+            stream = _CURRENT_STREAM(self._index)
+        if stream not in self._streams:
+            self._used_on(stream)
         sh = _ATTEND.pack(*self._head, width, *self._tail, row, *qs[:3], *os_[:3], *wi, *wo)
         _launch("e2s_cache_attend",
                 (self.workspace, q, pages, lengths, out, q_count, weights_in, weights_out),
