@@ -43,7 +43,9 @@ extern "C" {
  *   BASE    base * factor^(R/(R-2)) in place of base (R = 2: base)
  *   RAMP    by the turns r_j = original_len * f_j / (2 pi) that a pair makes over the
  *           original context: f_j / factor up to `low` turns, f_j from `high` turns on,
- *           linear in r_j between them
+ *           linear in r_j between them.  (Some implementations ramp linearly in the
+ *           pair's number j between the pairs of those turns.  A model trained so has other
+ *           frequencies in between, which no scaling here gives.)
  * Angles are reduced in 64 bits, so positions up to 2^31 keep the digits of their
  * angle; sine and cosine are those of a 32-bit angle within one turn.
  * ------------------------------------------------------------------------- */
@@ -116,7 +118,9 @@ E2S_API e2s_status e2s_rotate_positions(const e2s_rotary_shape* shape,
  * largest finite value (448 * 2^e).  So a block whose maximum grows as tokens are
  * appended, and rows that eviction regroups into other blocks, are rescaled exactly but
  * for values under 2^-13 of the block's maximum, below e4m3's normal range.  NaN
- * stays NaN; infinities are held as NaN.
+ * stays NaN; infinities are held as NaN.  Elements from 248 * 2^120 on (3.3e38) are held as
+ * 2^128.  A scale that the caller writes has to be a power of two in 2^-100 .. 2^120, too:
+ * attention reads its exponent alone.
  *   A sequence's tokens lie in the pages that its row of a page
  * table [B, max_pages] int32 names: token n in page pages[b, n / P], row n % P.  A page
  * belongs to one sequence while it is written.

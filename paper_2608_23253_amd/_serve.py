@@ -167,7 +167,8 @@ def rotary_plan(head_dim: int, rot_dim: Optional[int] = None, base: float = 1000
                 low: float = 1.0, high: float = 32.0, amplitude: float = 0.0,
                 sections=None) -> RotaryPlan:
     """The frequencies of e2s_rotate_positions (see e2s_rotary_spec): rot_dim leading
-    elements of a row turn (default: all).  scaling: "none", "linear", "base" or "ramp".
+    elements of a row turn (default: all).  scaling: "none", "linear", "base" or "ramp" (linear
+    in a pair's turns, not in its number).
     sections: numbers of pairs that turn by each of three positions, or None."""
     spec = RotarySpec(head_dim, head_dim if rot_dim is None else rot_dim,
                       ROTARY_LAYOUTS[layout] if isinstance(layout, str) else int(layout),
@@ -280,7 +281,8 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
 class PagedCache:
     """The 8-bit cache of one layer (e2s_cache): k, v [num_pages, Hkv, P, d]
     float8_e4m3fn and k_scale, v_scale [num_pages, Hkv] float32; a held value is its byte
-    times its block's scale.  Which sequence a page belongs to is the caller's page
+    times its block's scale, a power of two (2^-100 .. 2^120: of any other that the caller
+    puts there attention reads the exponent alone).  Which sequence a page belongs to is the caller's page
     table's to say."""
 
     def __init__(self, num_pages: int, num_kv_heads: int, head_dim: int, page_tokens: int = 64,

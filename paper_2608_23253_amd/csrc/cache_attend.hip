@@ -35,10 +35,11 @@
 //
 // Many rows (attend_rows_kernel): the waves take 16 or 32 rows each, widen the keys' and
 // values' operands once for all into LDS, and wait for each other twice a step.  2 sequences
-// of 2048 queries and keys, 28 heads: 150 us, 800 TFLOP/s counting the second term's
-// products; 16 ragged ones of up to 48 queries and 4200 keys: 44 us, where few workgroups
-// remain to hide a step's latencies (registers leave three waves a SIMD; all operands read
-// ahead from LDS, two waves a SIMD: 60).
+// of 2048 queries and keys, 28 heads, bf16: 145 us, 415 TFLOP/s of the 60 GFLOP that the mask
+// leaves, 620 counting the second term's products (f16, two query terms and 16 rows a wave: 188
+// us); 16 ragged ones of up to 48 queries and 4200 keys: 47 us before the join, where few
+// workgroups remain to hide a step's latencies (registers leave three waves a SIMD; all
+// operands read ahead from LDS, two waves a SIMD: 60).
 //
 // attend_finish_kernel joins the parts (21504 rows of up to 5: 6 us) and adds up few rows'
 // weights, attend_weights_kernel does where that is a launch of its own, and
@@ -1214,7 +1215,7 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(const AttendAr
 
 // The tokens' weights from many rows, whose sums lie in the workspace: the logits are made a
 // second time, since through memory they would cost 8 bytes per row and key (16 sequences of
-// up to 48 queries and 4200 keys, 28 heads: 183 us for the call, 85 so, 55 without weights).
+// up to 48 queries and 4200 keys, 28 heads: 183 us for the call, 82 so, 51 without weights).
 // A wave holds the operands of its 64 keys and walks over the rows, 16 at a time (32 keys: 93
 // us, 16: 110); a lane adds up what its row of each tile gives 16 keys, and the 16 lanes of a
 // key are summed at the end.  Reading and widening the queries and the exponentials bound it.
@@ -1450,6 +1451,9 @@ hipError_t launch_cache_attend(const e2s_cache& c, const e2s_cache_attend_shape&
     a.max_tokens = s.max_tokens;
     a.causal = s.causal;
     const double scale = s.scale != 0.0f ? s.scale : 1.0 / std::sqrt(static_cast<double>(c.head_dim));
+    // one rounding for both factors: every logit is off by at most 2^-24 of itself by it, which
+    // f32 queries show where logits are large (a weight by 2^-24 of its logit's distance from
+    // the maximum); a second factor would cost an operation per logit
     a.scale = static_cast<float>(scale * 1.4426950408889634 / kKeySize);
     if (s.dtype == E2S_DTYPE_F32) return launch_d<float>(a, p, s.batch, c.head_dim, st);
     if (s.dtype == E2S_DTYPE_F16) return launch_d<_Float16>(a, p, s.batch, c.head_dim, st);

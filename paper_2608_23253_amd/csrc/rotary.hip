@@ -6,7 +6,9 @@
 // 14.5 us, most of them from the last-level cache; one token's heads 3.6 us.  Sine and cosine depend on the token and the pair alone, not on the head, so
 // a workgroup takes a run of TT tokens of one sequence for all heads of q and k: its
 // threads first compute the TT * R/2 pairs (cos, sin) into LDS - the angle as turns,
-// p * f_j / (2 pi), in float64, of which only the fraction matters - and then each keeps
+// p * f_j / (2 pi), in float64, of which only the fraction matters, rounded to float32 (at most
+// pi 2^-25 of an angle within half a turn; float32 rows are 4.7e-8 off on the whole, 3.6e-8 with
+// sine and cosine of float64 angles) - and then each keeps
 // its pairs' values in registers while it walks over the heads.
 //
 // A unit is two chunks of W elements of a row: the first and second members of W pairs

@@ -256,7 +256,7 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     // the rows (16 or 32 each) and share the keys' operands in LDS.  Two tiles of rows keep a
     // wave that parts the keys busy with products, so from 17 rows on the rows are parted where
     // there are many keys, although half of the waves then have none: 4 queries of 28 heads
-    // (4 key heads) against 4 sequences of 16000 keys take 27 us so and 35 us, of 2000 keys 18
+    // (4 key heads) against 4 sequences of 16000 keys take 27 us so and 36 us, of 2000 keys 18
     // and 15.
     p.shared_rows = p.rows > 32 || (p.rows > 16 && B * G * s.max_tokens > 131072);
     const int64_t per_tile = p.shared_rows ? 16 * kAttendWaves : 16;
@@ -271,9 +271,9 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
     const int64_t units = B * G * p.row_groups;
     // Keys are split until 2048 workgroups fill the device, most of which have nothing to do
     // where sequences are of unequal lengths (16 of 300 to 4200 keys, up to 48 queries of 28
-    // heads: 60 us; 1536 workgroups: 74, 2560: 63).  Units of 32 rows to a wave are enough as
-    // they are: 4 sequences of 512 queries and 2000 keys, 32 heads take 121 us unsplit, 169
-    // and 178 in two and three parts.
+    // heads: 52 us; 1536 workgroups: 63, 2560: 56).  Units of 32 rows to a wave are enough as
+    // they are: 4 sequences of 512 queries and 2000 keys, 32 heads take 107 us unsplit, 153
+    // with 16 rows to a wave, which are split.
     int64_t per = p.shared_rows && p.tiles == 2 ? s.max_tokens
                                                 : (s.max_tokens * units + 2047) / 2048;
     // Short sequences: one workgroup of eight waves has all keys, and nothing is left to join.
@@ -296,7 +296,7 @@ AttendPlan attend_plan(const e2s_cache& c, const e2s_cache_attend_shape& s) {
         per = std::max<int64_t>(per, 4 * unit);
     } else {
         // Parts of fewer than 1024 keys are mostly their own beginning and end: there 1024
-        // workgroups are enough (200 sequences of 300 keys: 25 us, 38 in two parts).
+        // workgroups are enough (200 sequences of 300 keys: 26 us, 40 in two parts).
         per = std::max<int64_t>(
             per, std::min<int64_t>(1024, (s.max_tokens * units + 1023) / 1024));
         per = std::max<int64_t>(per, 2 * unit);
