@@ -282,8 +282,8 @@ class PagedCache:
     """The 8-bit cache of one layer (e2s_cache): k, v [num_pages, Hkv, P, d]
     float8_e4m3fn and k_scale, v_scale [num_pages, Hkv] float32; a held value is its byte
     times its block's scale, a power of two (2^-100 .. 2^120: of any other that the caller
-    puts there attention reads the exponent alone).  Which sequence a page belongs to is the caller's page
-    table's to say."""
+    puts there attention reads the exponent alone).  Which sequence a page belongs to is the
+    caller's page table's to say."""
 
     def __init__(self, num_pages: int, num_kv_heads: int, head_dim: int, page_tokens: int = 64,
                  device="cuda"):

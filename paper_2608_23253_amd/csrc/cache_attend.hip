@@ -61,7 +61,7 @@ constexpr float kRaise = 8.0f;                 // log2 by which a logit may pass
 // value, 2^128, is finite so, and so is a sum of values below 2^116 under 2^20 weights of up to
 // 2^kRaise.  The logits' scale and the division by the weights' sum give it back.
 constexpr int kKeyDown = 1, kValueDown = 16;
-constexpr float kKeySize = 1.0f / (1 << kKeyDown), kValueSize = 1.0f / (1 << kValueDown);
+constexpr float kKeySize = 1.0f / (1 << kKeyDown), kValueUp = 1 << kValueDown;
 
 typedef __bf16 bf16x8s __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4s __attribute__((ext_vector_type(4)));
@@ -154,7 +154,8 @@ __device__ __forceinline__ V load_stream(const uint8_t* p) {
 // unit, behind the lookup, it showed: 9.50 us for 9.43 with one sequence).
 template <int DOWN>
 __device__ __forceinline__ float lane_scale(float x, int lane) {
-    return __int_as_float(max(__builtin_amdgcn_readlane(__float_as_int(x), lane) - (DOWN << 23), 0));
+    const int bits = __builtin_amdgcn_readlane(__float_as_int(x), lane);
+    return __int_as_float(max(bits - (DOWN << 23), 0));
 }
 // Words whose bytes are 0x80 where w has a NaN (0x7F or 0xFF).
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
@@ -645,7 +646,7 @@ __global__ __launch_bounds__(64 * WAVES, TILES == 1 ? 4 : 2) void attend_kernel(
             }
             const int64_t line = (b * a.G + g) * static_cast<int64_t>(a.rows) + row;
             if (WAVES == 8 || a.splits == 1) {           // eight waves: never split
-                const float inv = total > 0.0f || total != total ? 1.0f / kValueSize / total : 0.0f;
+                const float inv = total > 0.0f || total != total ? kValueUp / total : 0.0f;
                 const int t = row / a.group;
                 T* to = static_cast<T*>(a.out) + b * a.os[0] +
                         (g * a.group + row - t * a.group) * a.os[1] + t * a.os[2] + d0;
@@ -989,7 +990,7 @@ __global__ __launch_bounds__(kThreads, TILES == 1 && Terms<T>::n == 1 ? 3 : 2) v
         if (row >= row_end) continue;
         const int64_t line = (b * a.G + g) * static_cast<int64_t>(a.rows) + row;
         if (TILES == 2 || a.splits == 1) {           // 32 rows a wave: never split
-            const float inv = total > 0.0f || total != total ? 1.0f / kValueSize / total : 0.0f;
+            const float inv = total > 0.0f || total != total ? kValueUp / total : 0.0f;
             const int t = row / a.group;
             T* to = static_cast<T*>(a.out) + b * a.os[0] +
                     (g * a.group + row - t * a.group) * a.os[1] + t * a.os[2] + 4 * g4 * kDims;
@@ -1047,7 +1048,7 @@ __device__ __forceinline__ JoinRow join_row(const AttendArgs& a, uint32_t line, 
 template <typename T, int N>
 __device__ __forceinline__ void join_out(const AttendArgs& a, const JoinRow& r, uint32_t line,
                                          int dim, float m, float total, const float (&y)[N]) {
-    const float inv = total > 0.0f || total != total ? 1.0f / kValueSize / total : 0.0f;
+    const float inv = total > 0.0f || total != total ? kValueUp / total : 0.0f;
     T* to = static_cast<T*>(a.out) + r.b * a.os[0] + r.head * a.os[1] + r.t * a.os[2] + dim;
     Run<T, N> z;
 #pragma unroll
