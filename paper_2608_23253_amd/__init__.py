@@ -12,6 +12,8 @@ from ._lib import (VARIANTS, CompactShape, E2SError, Image, Params, Pruner, QKVi
                    workspace_size)
 from ._serve import (CacheAttention, PagedCache, RotaryPlan, cache_append, cache_attend,
                      cache_evict, rotary_plan, rotate_positions)
+from ._step import (Cache4Attention, PagedCache4, cache4_append, cache4_attend, cache4_read,
+                    norm_rotate, norm_rotate_backward)
 
 __all__ = ["VARIANTS", "CompactShape", "E2SError", "Image", "Params", "Pruner", "QKViews",
            "RaggedPruner", "RaggedShape", "Shape", "StagePruner", "compact_tokens",
@@ -20,4 +22,5 @@ __all__ = ["VARIANTS", "CompactShape", "E2SError", "Image", "Params", "Pruner", 
            "packed_images", "prune", "prune_noalloc", "prune_ragged", "prune_stage", "prune_views", "qk_views",
            "score_heads", "spatial_select", "workspace_size", "CacheAttention", "PagedCache",
            "RotaryPlan", "cache_append", "cache_attend", "cache_evict", "rotary_plan",
-           "rotate_positions"]
+           "rotate_positions", "Cache4Attention", "PagedCache4", "cache4_append",
+           "cache4_attend", "cache4_read", "norm_rotate", "norm_rotate_backward"]

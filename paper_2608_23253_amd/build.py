@@ -24,7 +24,8 @@ LIB = os.path.join(PKG, "libe2s.so")
 SOURCES = ["e2s_validate.cpp", "e2s_api.hip", "score.hip", "score_prob.hip", "layer.hip",
            "fuse.hip", "select.hip", "compact.hip", "read_probe.hip", "serve_validate.cpp",
            "serve_api.hip", "rotary.hip", "cache_append.hip", "cache_attend.hip",
-           "cache_evict.hip"]
+           "cache_evict.hip", "step_validate.cpp", "step_api.hip", "norm_rotate.hip",
+           "cache4_append.hip", "cache4_attend.hip"]
 
 ARCH = "gfx950"
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-Wno-unused-parameter",

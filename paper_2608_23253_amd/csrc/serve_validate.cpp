@@ -11,6 +11,8 @@ namespace {
 constexpr double kBig = static_cast<double>(std::numeric_limits<int64_t>::max() / 16);
 constexpr int64_t kMaxStride = std::numeric_limits<int64_t>::max() / 64;
 
+}  // namespace
+
 bool known_dtype(int32_t t) {
     return t == E2S_DTYPE_F32 || t == E2S_DTYPE_BF16 || t == E2S_DTYPE_F16;
 }
@@ -36,8 +38,6 @@ e2s_status check_strides(const int64_t* st, const int64_t* counts, int n, int64_
         const e2s_status st__ = (expr);        \
         if (st__ != E2S_OK) return st__;       \
     } while (0)
-
-}  // namespace
 
 e2s_status check_rotary_spec(const e2s_rotary_spec* s) {
     if (s == nullptr) return E2S_ERR_NULL_POINTER;
@@ -157,13 +157,11 @@ e2s_status check_cache(const e2s_cache* c) {
     return E2S_OK;
 }
 
-namespace {
 e2s_status check_table(int64_t batch, int64_t max_pages, int64_t stride) {
     if (max_pages < 1) return E2S_ERR_BAD_SHAPE;
     const int64_t counts[1] = {batch};
     return check_strides(&stride, counts, 1, max_pages, 0, 0, 4);
 }
-}  // namespace
 
 e2s_status check_append(const e2s_cache& c, const e2s_cache_append_shape* s) {
     if (s == nullptr) return E2S_ERR_NULL_POINTER;

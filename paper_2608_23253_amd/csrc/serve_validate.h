@@ -12,6 +12,12 @@ namespace e2s {
 
 constexpr int64_t kMaxCachedTokens = 1 << 20;   // per sequence
 
+bool known_dtype(int32_t t);
+// Strides of n dimensions of rows of `row` elements of `bytes` each (see the definition).
+e2s_status check_strides(const int64_t* st, const int64_t* counts, int n, int64_t row, int least,
+                         int64_t align, int bytes);
+e2s_status check_table(int64_t batch, int64_t max_pages, int64_t stride);
+
 e2s_status check_rotary_spec(const e2s_rotary_spec* s);
 // Frequencies, axes and amplitude of a checked spec.
 void fill_rotary_plan(const e2s_rotary_spec& s, e2s_rotary_plan* p);
