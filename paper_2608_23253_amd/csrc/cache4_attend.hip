@@ -99,8 +99,9 @@ __device__ __forceinline__ float exponent_scale(int e) { return __int_as_float(e
 
 // Four values to a word of e4m3 bytes at a scale; the values become what that leaves of them.
 template <bool LAST>
-__device__ __forceinline__ int take_term(float (&x)[4], float scale) {
-    s16x2 w = {0, 0};
+__device__ __forceinline__ int take_term(f32x4& x, float scale) {
+    s16x2 w;
+    asm volatile("" : "=v"(w));      // any register: both halves are written
     w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[0], x[1], scale, false);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[2], x[3], scale, true);
     const uint32_t bits = __builtin_bit_cast(uint32_t, w);
@@ -154,41 +155,46 @@ __device__ __forceinline__ f32x4 value_product(int i, const u32x4& a, const i32x
     }
 }
 
-__device__ __forceinline__ float across_rows(float v) {      // the maximum over a column's lanes
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+// (the compiler would quieten every operand of its own first)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
-// 16 of the cache's bytes; read once: past the caches.
-template <bool ONCE>
-__device__ __forceinline__ u32x4 load_keys(const uint8_t* p) {
-    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-    else return *reinterpret_cast<const u32x4*>(p);
+// The maximum over a column's lanes, g = 0 .. 3: rows of 16 lanes change places with their
+// neighbours, then halves of the wave.
+__device__ __forceinline__ float across_rows(float v) {
+    typedef unsigned int u32x2a __attribute__((ext_vector_type(2)));
+    u32x2a p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(p.x), __uint_as_float(p.y));
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p.x), __uint_as_float(p.y));
 }
 
 template <typename T, int N> struct alignas(N * sizeof(T) < 16 ? N * sizeof(T) : 16) Run4 {
     T x[N];
 };
 
-// WAVES waves, ROW_WAVES of them along the rows (16 each), the others along the keys.
-template <typename T, int D, int WAVES, int ROW_WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel(
+// 16 rows to a workgroup, whose waves part its keys.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attend4_kernel(
     const Attend4Args a) {
     constexpr int kQ = Terms4<T>::q, kP = Terms4<T>::p;
     constexpr int kHalves = D == 128 ? 1 : 2;            // terms of a product's k
     constexpr int kQm = (kQ + kHalves - 1) / kHalves;    // key products of a tile
     constexpr int kDims = D / kTile;
-    constexpr int kKeyWaves = WAVES / ROW_WAVES;
     constexpr int kPad = D + 4;
     // the queries' operands; the waves' outputs at the end
     __shared__ union {
-        i32x4 q[ROW_WAVES][kQm][2][64];
-        float out[kKeyWaves > 1 ? WAVES : 1][kTile][kPad];
+        i32x4 q[kQm][2][64];
+        float out[WAVES > 1 ? WAVES : 1][kTile][kPad];
     } lds;
     __shared__ float top_of[WAVES][kTile], sum_of[WAVES][kTile];
 
     uint32_t id = blockIdx.x;
-    const int rg = static_cast<int>(id % static_cast<uint32_t>(a.row_groups));
+    // (causal: the last rows, which see the most, first)
+    const int rg = a.row_groups - 1 - static_cast<int>(id % static_cast<uint32_t>(a.row_groups));
     id /= static_cast<uint32_t>(a.row_groups);
     const int split = static_cast<int>(id % static_cast<uint32_t>(a.splits));
     id /= static_cast<uint32_t>(a.splits);
@@ -196,39 +202,35 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
     const int64_t b = id / static_cast<uint32_t>(a.G);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row_wave = wave % ROW_WAVES, key_wave = wave / ROW_WAVES;
     const int n16 = lane & 15, g4 = lane >> 4;
 
     const int len = length_of(a, b), count = count_of(a, b);
-    const int group0 = rg * kTile * ROW_WAVES;
-    const int group_end = min(group0 + kTile * ROW_WAVES, count * a.group);
-    if (group0 >= group_end) return;
+    const int row0 = rg * kTile;
+    const int row_end = min(row0 + kTile, count * a.group);
+    if (row0 >= row_end) return;
+    // what the first row and the last row see
+    const int least = seen_by(a, len, count, row0 / a.group);
+    const int most = seen_by(a, len, count, (row_end - 1) / a.group);
     const int64_t key_begin = split * a.chunk;
-    if (split > 0 && key_begin >= seen_by(a, len, count, (group_end - 1) / a.group)) return;
-
-    // this wave's rows: what its first row and its last row see
-    const int row0 = group0 + row_wave * kTile;
-    const int row_end = min(row0 + kTile, group_end);
-    const bool any_row = row0 < row_end;
-    const int least = any_row ? seen_by(a, len, count, row0 / a.group) : 0;
-    const int most = any_row ? seen_by(a, len, count, (row_end - 1) / a.group) : 0;
+    if (split > 0 && key_begin >= most) return;
     const int row = row0 + n16;
     const bool live = row < row_end;
     const int at_t = live ? row / a.group : 0, at_h = live ? row - at_t * a.group : 0;
     // rows that do not exist see everything, so that they mask nothing
     const int limit = live ? seen_by(a, len, count, at_t) : a.max_tokens;
-    // and this wave's keys
-    const int64_t quarter = a.chunk / kKeyWaves;
-    const int64_t wave_begin = key_begin + key_wave * quarter;
-    const int w0 = static_cast<int>(min(wave_begin, static_cast<int64_t>(most)));
-    const int w1 = static_cast<int>(min(wave_begin + quarter, static_cast<int64_t>(most)));
+    // this wave's keys: an equal share of the steps that the rows see
+    const int begin = static_cast<int>(min(key_begin, static_cast<int64_t>(most)));
+    const int end_of = static_cast<int>(min(key_begin + a.chunk, static_cast<int64_t>(most)));
+    const int share = ((end_of - begin + kStep4 - 1) / kStep4 + WAVES - 1) / WAVES * kStep4;
+    const int w0 = min(begin + wave * share, end_of);
+    const int w1 = min(w0 + share, end_of);
 
-    // Queries as operands: the first wave of each 16 rows lays them out.  Lane (n, g4) holds
+    // Queries as operands: the first wave lays them out.  Lane (n, g4) holds
     // elements lo .. lo + 15 and hi .. hi + 15 of row n; d = 64: the same twice, of two terms.
     int qs[(kQ + 3) / 4 + 1];                            // scales of the terms, a byte each
     {
         const int lo = 16 * g4, hi = D == 128 ? 64 + 16 * g4 : lo;
-        float x[8][4];
+        f32x4 x[8];
         const T* src = static_cast<const T*>(a.q) + b * a.qs[0] +
                        (static_cast<int64_t>(g) * a.group + at_h) * a.qs[1] + at_t * a.qs[2];
 #pragma unroll
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
 #pragma unroll
         for (int i = 0; i < kQm; ++i)
             qs[i >> 2] |= (mine - 4 * kHalves * i) << (8 * (i & 3));
-        if (key_wave == 0) {
+        if (wave == 0) {
 #pragma unroll
             for (int i = 0; i < kQm * kHalves; ++i) {
                 i32x4 t[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -272,86 +274,83 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
                     }
                 }
                 if constexpr (kHalves == 1) {
-                    lds.q[row_wave][i][0][lane] = t[0];
-                    lds.q[row_wave][i][1][lane] = t[1];
+                    lds.q[i][0][lane] = t[0];
+                    lds.q[i][1][lane] = t[1];
                 } else {
-                    lds.q[row_wave][i >> 1][i & 1][lane] = t[0];
+                    lds.q[i >> 1][i & 1][lane] = t[0];
                 }
             }
         }
     }
     __syncthreads();
 
-    // Lane l looks up the page of group l (32 keys) of a segment of 64.
+    // Lane l looks up group l (32 keys) of a segment of 64: its page (-1: none), the byte offsets
+    // of its keys and its values, and the number of its first token and head among all.  (Groups
+    // without a page read the first page's, unused.)
     constexpr int kSegment = 64 * kGroup4;
-    int page = -1;
+    struct Segment {
+        int page;
+        int64_t k, v, token;
+    };
+    const int64_t head = static_cast<int64_t>(g) * (D / 2) << a.page_shift;
     auto look_up = [&](int seg) {
-        const int key = seg + lane * kGroup4;
-        page = -1;
-        if (key < w1) page = a.pages[b * a.pages_stride + (key >> a.page_shift)];
-        if (page < 0 || page >= a.num_pages) page = -1;
+        Segment w;
+        const int key = seg + lane * kGroup4, row = key & (a.P - 1);
+        int pg = -1;
+        if (key < w1) pg = a.pages[b * a.pages_stride + (key >> a.page_shift)];
+        w.page = pg < a.num_pages ? max(pg, -1) : -1;
+        const int64_t at = max(w.page, 0);
+        w.k = at * a.k_page + head + row * (D / 2);
+        w.v = at * a.v_page + head + row * (D / 2);
+        w.token = ((at * a.G + g) << a.page_shift) + row;
+        return w;
+    };
+    auto from_lane = [&](int64_t x, int index) {
+        const int lo = __builtin_amdgcn_ds_bpermute(index, static_cast<int>(x));
+        const int hi = __builtin_amdgcn_ds_bpermute(index, static_cast<int>(x >> 32));
+        return static_cast<int64_t>(hi) << 32 | static_cast<uint32_t>(lo);
     };
     // A step's operands, as loaded.
     u32x4 kx[8], vx[kDims], vs[4];
     uint32_t ks[2];
-    const int page_mask = a.P - 1;
     // lane constants: of its keys' rows, their scales, its value rows, and the values' scales
-    const int m16 = n16;
-    const int k_tok = 16 * (m16 >> 2 & 1) + (m16 & 3);
-    const int k_off = k_tok * (D / 2) + (D == 128 ? g4 : g4 & 1) * 16;
-    const int ks_off = (m16 >> 2 & 1) * (D / 2) +
-                       ((m16 & 3) * (D / 32) + (D == 128 ? g4 : g4 & 1)) * 4;
-    const int v_off = m16 * 16;
-    const int vs_off = 16 * (g4 & 1);
-    // Of the step's four groups of 32 keys: their pages (-1: none).
-    struct Where {
-        int key, p0, p1, p2, p3;
-    };
-    auto where = [&](int key, int seg) {
-        const int i = (key - seg) >> 5;
-        return Where{key, __builtin_amdgcn_readlane(page, i),
-                     __builtin_amdgcn_readlane(page, i + 1),
-                     __builtin_amdgcn_readlane(page, i + 2),
-                     __builtin_amdgcn_readlane(page, i + 3)};
-    };
-    // Byte offsets of a group's keys and values (by page stride), and of its tokens among all.
-    // (Groups without a page read the first one's, unused.)
-    const int64_t head = static_cast<int64_t>(g) * (D / 2) << a.page_shift;
-    auto bytes_at = [&](int pg, int key, int64_t stride) {
-        return max(pg, 0) * stride + head + (key & page_mask) * (D / 2);
-    };
-    auto token_at = [&](int pg, int key) {
-        return ((static_cast<int64_t>(max(pg, 0)) * a.G + g) << a.page_shift) + (key & page_mask);
-    };
-    const bool k_odd = (m16 & 8) != 0, v_odd = (g4 & 1) != 0, v_far = (g4 & 2) != 0;
-    auto fetch_half = [&](int f, int pa, int pb, int key) {
-        const int64_t ka = bytes_at(pa, key, a.k_page), kb = bytes_at(pb, key + 32, a.k_page);
-        const int64_t sa = token_at(pa, key) * (D / 32), sb = token_at(pb, key + 32) * (D / 32);
-        const uint8_t* p = a.k + (k_odd ? kb : ka) + k_off;
+    const int k_tok = 16 * (n16 >> 2 & 1) + (n16 & 3);
+    const int k_block = D == 128 ? g4 : g4 & 1;
+    const uint8_t* const k_lane = a.k + k_tok * (D / 2) + k_block * 16;
+    const uint8_t* const ks_lane =
+        a.k_scale + (n16 >> 2 & 1) * (D / 2) + ((n16 & 3) * (D / 32) + k_block) * 4;
+    const uint8_t* const v_lane = a.v + n16 * 16;
+    const uint16_t* const vs_lane = a.v_scale + 16 * (g4 & 1);
+    const bool v_far = (g4 & 2) != 0;
+    // the lane (times 4) of its keys', its values' and its values' scales' first group in a segment
+    const int k_from = (n16 >> 3) * 4, v_from = g4 * 4, vs_from = (g4 >> 1) * 4;
+    auto fetch_k = [&](const Segment& w, int key) {      // key: of the segment
+        const int at = (key >> 5) * 4 + k_from;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) kx[4 * f + u] = load_keys<ROW_WAVES == 1>(p + u * 2 * D);
-        ks[f] = *reinterpret_cast<const uint32_t*>(a.k_scale + (k_odd ? sb : sa) + ks_off);
-    };
-    auto fetch_k = [&](const Where& w) {
-        fetch_half(0, w.p0, w.p1, w.key);
-        fetch_half(1, w.p2, w.p3, w.key + 64);
-    };
-    auto fetch_v = [&](const Where& w) {
-        const int64_t v0 = bytes_at(w.p0, w.key, a.v_page), v1 = bytes_at(w.p1, w.key + 32, a.v_page);
-        const int64_t v2 = bytes_at(w.p2, w.key + 64, a.v_page);
-        const int64_t v3 = bytes_at(w.p3, w.key + 96, a.v_page);
-        const int64_t va = v_odd ? v1 : v0, vb = v_odd ? v3 : v2;
-        const uint8_t* p = a.v + (v_far ? vb : va) + v_off;
+        for (int f = 0; f < 2; ++f) {
+            const uint8_t* p = k_lane + from_lane(w.k, at + 8 * f);
 #pragma unroll
-        for (int j = 0; j < kDims; ++j) vx[j] = load_keys<ROW_WAVES == 1>(p + j * 256);
-        const int64_t s0 = token_at(w.p0, w.key), s1 = token_at(w.p1, w.key + 32);
-        const int64_t s2 = token_at(w.p2, w.key + 64), s3 = token_at(w.p3, w.key + 96);
-        const u32x4* sa = reinterpret_cast<const u32x4*>(a.v_scale + (v_far ? s1 : s0) + vs_off);
-        const u32x4* sb = reinterpret_cast<const u32x4*>(a.v_scale + (v_far ? s3 : s2) + vs_off);
-        vs[0] = sa[0];
-        vs[1] = sa[1];
-        vs[2] = sb[0];
-        vs[3] = sb[1];
+            for (int u = 0; u < 4; ++u)
+                kx[4 * f + u] = *reinterpret_cast<const u32x4*>(p + u * 2 * D);
+            ks[f] = *reinterpret_cast<const uint32_t*>(ks_lane +
+                                                       from_lane(w.token, at + 8 * f) * (D / 32));
+        }
+    };
+    auto fetch_v = [&](const Segment& w, int key) {
+        const int at = (key >> 5) * 4;
+        const uint8_t* p = v_lane + from_lane(w.v, at + v_from);
+        const u32x4* s[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+            s[f] = reinterpret_cast<const u32x4*>(vs_lane +
+                                                  from_lane(w.token, at + vs_from + 8 * f));
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            vs[2 * f] = s[f][0];
+            vs[2 * f + 1] = s[f][1];
+        }
+#pragma unroll
+        for (int j = 0; j < kDims; ++j) vx[j] = *reinterpret_cast<const u32x4*>(p + j * 256);
     };
 
     f32x4 o[kDims];
@@ -359,41 +358,36 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
 #pragma unroll
     for (int j = 0; j < kDims; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // One step of 128 keys.  `whole`: every row sees every key of it.
-    auto step = [&](auto whole_tag, int key, const Where& now, const Where& next) {
-        constexpr bool kWhole = decltype(whole_tag)::value;
+    f32x4 s[8];                          // logits before their scale
+    // The parts of a step of 128 keys.
+    auto read_query = [&](int i) {
         // an index that the compiler cannot know keeps the queries' reads in the loop
         int my = lane;
         asm volatile("" : "+v"(my));
-        f32x4 s[8];
+        const i32x4 q0 = lds.q[i][0][my], q1 = lds.q[i][1][my];
+        return i32x8{q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+    };
+    auto logit_term = [&](int i, int t, const i32x8& q, const f32x4& c) {
+        return key_product(i, t & 3, kx[t], q, c, static_cast<int>(ks[t >> 2]), qs[i >> 2]);
+    };
+    // Lane (n, g4): s[4 f + u][r] is key 64 f + 16 g4 + 4 u + r; -inf where it is not seen.
+    auto mask = [&](const Segment& w, int seg, int key) {
+        int page[2];                             // of the lane's two groups
 #pragma unroll
-        for (int t = 0; t < 8; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = kQm - 1; i >= 0; --i) {
-            const i32x4 q0 = lds.q[row_wave][i][0][my], q1 = lds.q[row_wave][i][1][my];
-            const i32x8 q = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-                s[t] = key_product(i, t & 3, kx[t], q, s[t], static_cast<int>(ks[t >> 2]),
-                                   qs[i >> 2]);
-        }
-        fetch_k(next);
-        // Logits to weights.  Lane (n, g4): s[4 f + u][r] is key 64 f + 16 g4 + 4 u + r.
-        float y[8][4];
-        float mx = -kInf;
+        for (int f = 0; f < 2; ++f)
+            page[f] = __builtin_amdgcn_ds_bpermute((key >> 5) * 4 + vs_from + 8 * f, w.page);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            const bool there = t < 4 ? (v_far ? now.p1 : now.p0) >= 0 : (v_far ? now.p3 : now.p2) >= 0;
+            const int end = page[t >> 2] >= 0 ? limit : 0;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                y[t][r] = s[t][r];
-                if constexpr (!kWhole) {
-                    const int kk = key + 64 * (t >> 2) + 16 * g4 + 4 * (t & 3) + r;
-                    if (!there || kk >= limit) y[t][r] = -kInf;
-                }
-                mx = fmaxf(mx, y[t][r]);
-            }
+            for (int r = 0; r < 4; ++r)
+                if (seg + key + 64 * (t >> 2) + 16 * g4 + 4 * (t & 3) + r >= end) s[t][r] = -kInf;
         }
+    };
+    auto raise = [&]() {
+        float mx = -kInf;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) mx = max3(mx, s[i >> 2][i & 3], s[i >> 2][(i & 3) + 1]);
         mx *= a.scale;
         if (__ballot(mx > top + kRaise)) {
             // (a whole number: what is taken from the logits is exact)
@@ -406,60 +400,84 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
 #pragma unroll
             for (int j = 0; j < kDims; ++j) o[j] *= shrink;
         }
-        float pm = 0.0f;
+    };
+    // One step, of key `key` of the segment that starts at seg, with key `ahead` behind it.
+    // `whole`: every row sees every key of it.
+    auto step = [&](auto whole_tag, const Segment& now, int seg, int key, int ahead) {
+        constexpr bool kWhole = decltype(whole_tag)::value;
+        fetch_v(now, key);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = kQm - 1; i >= 0; --i) {
+            const i32x8 q = read_query(i);
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                s[t] = logit_term(i, t, q, i == kQm - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t]);
+        }
+        // (the loads take the registers of what they follow, and no others)
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_k(now, ahead);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!kWhole) mask(now, seg, key);
+        raise();
+        // logits to weights times their values' scales
+        uint32_t pm = 0;                         // the largest: their bits are ordered as they are
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             const uint32_t w2[2] = {vs[t >> 1][2 * (t & 1)], vs[t >> 1][2 * (t & 1) + 1]};
             float part[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bool masked = !kWhole && y[t][r] == -kInf;
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(y[t][r], a.scale, -base));
-                part[r] = p;
+                const float x = s[t][r];
+                part[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale, -base));
                 const float f = r & 1 ? bf16hi(w2[r >> 1]) : bf16lo(w2[r >> 1]);
-                y[t][r] = masked ? 0.0f : p * f;
-                pm = fmaxf(pm, y[t][r]);
+                // (what is not seen may have any scale)
+                s[t][r] = !kWhole && x == -kInf ? 0.0f : part[r] * f;
             }
+            pm = max(max(pm, __float_as_uint(s[t][0])), __float_as_uint(s[t][1]));
+            pm = max(max(pm, __float_as_uint(s[t][2])), __float_as_uint(s[t][3]));
             sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
-        pm = across_rows(pm);
-        const int e = term_exponent(pm);
+        __builtin_amdgcn_sched_barrier(0);
+        const int e = term_exponent(across_rows(__uint_as_float(pm)));
         int es = 0, es2 = 0;
 #pragma unroll
         for (int i = 0; i < kP; ++i) (i < 4 ? es : es2) |= (e - 4 * i) << (8 * (i & 3));
+        // A term's products beside the conversion of the next one's words: the vector unit and
+        // the matrix unit work side by side where a wave's instructions alternate, which the
+        // scheduling fences keep them to.
+        i32x8 w[2];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) w[0][t] = take_term<false>(s[t], exponent_scale(e));
 #pragma unroll
         for (int i = 0; i < kP; ++i) {
-            const float sc = exponent_scale(e - 4 * i);
-            i32x8 w;
+            const float sc = exponent_scale(e - 4 * (i + 1));
 #pragma unroll
-            for (int t = 0; t < 8; ++t)
-                w[t] = i + 1 < kP ? take_term<false>(y[t], sc) : take_term<true>(y[t], sc);
-#pragma unroll
-            for (int j = 0; j < kDims; ++j)
-                o[j] = value_product(i, vx[j], w, o[j], i < 4 ? es : es2);
+            for (int j = 0; j < 8; ++j) {
+                if (j < kDims) o[j] = value_product(i, vx[j], w[i & 1], o[j], i < 4 ? es : es2);
+                if (i + 1 < kP)
+                    w[(i + 1) & 1][j] =
+                        i + 2 < kP ? take_term<false>(s[j], sc) : take_term<true>(s[j], sc);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        fetch_v(next);
+        __builtin_amdgcn_sched_barrier(0);
     };
 
-    if (w0 < w1) {
-        look_up(w0);
-        Where now = where(w0, w0);
-        fetch_k(now);
-        fetch_v(now);
-        int seg = w0;
-        for (int key = w0; key < w1; key += kStep4) {
-            int ahead = key + kStep4;
-            if (ahead >= w1) ahead = key;            // nothing follows: the same again, unused
-            if (ahead - seg >= kSegment) {
-                seg = ahead;
-                look_up(seg);
-            }
-            const Where next = where(ahead, seg);
-            const bool paged = (now.p0 | now.p1 | now.p2 | now.p3) >= 0;
-            if (paged && key + kStep4 <= least) step(std::true_type{}, key, now, next);
-            else step(std::false_type{}, key, now, next);
-            now = next;
-        }
+    // A segment's steps that every row sees whole, all pages there, come first, by code that
+    // masks nothing; the others by code that does.
+    for (int seg = w0; seg < w1; seg += kSegment) {
+        const Segment now = look_up(seg);
+        fetch_k(now, 0);
+        const int end = min(w1 - seg, kSegment);
+        const bool paged = __ballot(lane * kGroup4 < end && now.page < 0) == 0;
+        const int whole_end = paged ? min(end, least - seg) : 0;
+        // (behind the last step nothing follows: the same again, unused)
+        auto ahead = [&](int key) { return key + kStep4 < end ? key + kStep4 : key; };
+        int key = 0;
+        for (; key + kStep4 <= whole_end; key += kStep4)
+            step(std::true_type{}, now, seg, key, ahead(key));
+        for (; key < end; key += kStep4) step(std::false_type{}, now, seg, key, ahead(key));
     }
 
     sum += __shfl_xor(sum, 16);
@@ -487,7 +505,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
             }
         }
     };
-    if constexpr (kKeyWaves == 1) {
+    if constexpr (WAVES == 1) {
         // lane (n, g4) holds dimensions 16 j + 4 g4 .. of row n
         if (live) {
 #pragma unroll
@@ -503,9 +521,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
             sum_of[wave][n16] = sum;
         }
         __syncthreads();
-        float all = top_of[row_wave][n16];
+        float all = top_of[0][n16];
 #pragma unroll
-        for (int w = 1; w < kKeyWaves; ++w) all = fmaxf(all, top_of[row_wave + w * ROW_WAVES][n16]);
+        for (int w = 1; w < WAVES; ++w) all = fmaxf(all, top_of[w][n16]);
         const float f = top == -kInf ? 0.0f : top == all ? 1.0f : __builtin_amdgcn_exp2f(top - all);
 #pragma unroll
         for (int j = 0; j < kDims; ++j) {
@@ -513,22 +531,20 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
             *reinterpret_cast<f32x4*>(&lds.out[wave][n16][kTile * j + 4 * g4]) = y;
         }
         __syncthreads();
-        // the key waves of 16 rows share what is left
-        for (int i = key_wave * 64 + lane; i < kTile * D / 4; i += 64 * kKeyWaves) {
+        for (int i = threadIdx.x; i < kTile * D / 4; i += 64 * WAVES) {
             const int r = i / (D / 4), d0 = i % (D / 4) * 4;
             if (row0 + r >= row_end) continue;
-            float m = top_of[row_wave][r];
+            float m = top_of[0][r];
 #pragma unroll
-            for (int w = 1; w < kKeyWaves; ++w) m = fmaxf(m, top_of[row_wave + w * ROW_WAVES][r]);
+            for (int w = 1; w < WAVES; ++w) m = fmaxf(m, top_of[w][r]);
             float total = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kKeyWaves; ++w) {
-                const int from = row_wave + w * ROW_WAVES;
+            for (int w = 0; w < WAVES; ++w) {
                 // without a maximum a sum is 0, or NaN, which stays
-                const float tw = top_of[from][r];
-                total += sum_of[from][r] *
+                const float tw = top_of[w][r];
+                total += sum_of[w][r] *
                          (tw == m || tw == -kInf ? 1.0f : __builtin_amdgcn_exp2f(tw - m));
-                const f32x4 x = *reinterpret_cast<const f32x4*>(&lds.out[from][r][d0]);
+                const f32x4 x = *reinterpret_cast<const f32x4*>(&lds.out[w][r][d0]);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) y[k] += x[k];
             }
@@ -537,48 +553,77 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend4_kernel
     }
 }
 
-// The parts of a row joined, 4 dimensions to a thread.  A part is there where its first key is
-// seen by the workgroup that wrote it; parts whose keys this row does not see hold a maximum
-// of -inf (and zeros, or NaN, which only rows that do not exist make).
-template <typename T, int D>
+// The parts of a row joined, 4 dimensions to a thread, PARTS threads to every 4 dimensions: one
+// takes the first of them, and every PARTS-th behind it.  A part is there where its first key is
+// seen by the workgroup that wrote it; parts whose keys this row does not see hold a maximum of
+// -inf (and zeros, or NaN, which only rows that do not exist make).
+template <typename T, int D, int PARTS>
 __global__ __launch_bounds__(256) void attend4_join_kernel(const Attend4Args a, uint32_t lines) {
-    constexpr int kLanes = D / 4;
-    const uint32_t line = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
-    if (line >= lines) return;
-    const int d0 = static_cast<int>(threadIdx.x % kLanes) * 4;
-    const uint32_t bg = line / static_cast<uint32_t>(a.rows);
-    const int row = static_cast<int>(line - bg * static_cast<uint32_t>(a.rows));
+    constexpr int kLanes = D / 4, kLines = 256 / (kLanes * PARTS);
+    __shared__ float tops[PARTS > 1 ? PARTS : 1][kLines][kLanes];
+    __shared__ float sums[PARTS > 1 ? PARTS : 1][kLines][kLanes];
+    __shared__ f32x4 outs[PARTS > 1 ? PARTS : 1][kLines][kLanes];
+    const int lane = threadIdx.x % kLanes, part0 = threadIdx.x / kLanes % PARTS;
+    const int which = threadIdx.x / (kLanes * PARTS), d0 = lane * 4;
+    const uint32_t line = blockIdx.x * kLines + which;
+    const uint32_t bg = line < lines ? line / static_cast<uint32_t>(a.rows) : 0;
+    const int row = line < lines ? static_cast<int>(line - bg * static_cast<uint32_t>(a.rows)) : 0;
     const int64_t b = bg / static_cast<uint32_t>(a.G);
     const int g = static_cast<int>(bg - static_cast<uint32_t>(b) * a.G);
     const int t = row / a.group;
     const int len = length_of(a, b), count = count_of(a, b);
-    if (t >= count) return;
-    const int64_t sees = seen_by(a, len, count, t);
-    const int parts = static_cast<int>((sees + a.chunk - 1) / a.chunk);
+    const bool live = line < lines && t < count;
+    const int chunk = static_cast<int>(a.chunk);
+    const int parts = live ? (seen_by(a, len, count, t) + chunk - 1) / chunk : 0;     // <= splits
     const int64_t first = static_cast<int64_t>(line) * a.splits;
-    float m = -kInf;
-    for (int i = 0; i < parts; ++i) m = fmaxf(m, a.part_max[first + i]);
-    float total = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < parts; i0 += 4) {
+    float m = -kInf, total = 0.0f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = part0; i0 < parts; i0 += 4 * PARTS) {
         f32x4 x[4];
         float pm[4], ps[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {            // loads of four parts under way at once
-            const int64_t at = first + min(i0 + j, parts - 1);
+            const int i = i0 + j * PARTS;
+            const int64_t at = first + min(i, parts - 1);
             x[j] = *reinterpret_cast<const f32x4*>(a.part_out + at * D + d0);
-            pm[j] = a.part_max[at];
-            ps[j] = a.part_sum[at];
+            pm[j] = i < parts ? a.part_max[at] : -kInf;
+            ps[j] = i < parts ? a.part_sum[at] : 0.0f;
         }
+        // (maxima are whole numbers: their distances' powers of two are exact)
+        const float up = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m);
+        const float old = m == up ? 1.0f : __builtin_amdgcn_exp2f(m - up);
+        total *= old;
+        y *= old;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (i0 + j >= parts) break;
-            const float f =
-                pm[j] == m || pm[j] == -kInf ? 1.0f : __builtin_amdgcn_exp2f(pm[j] - m);
+            if (i0 + j * PARTS >= parts) break;
+            // without a maximum sum and output are 0, or NaN, which stays
+            const float f = pm[j] == up || pm[j] == -kInf ? 1.0f
+                                                          : __builtin_amdgcn_exp2f(pm[j] - up);
             total += ps[j] * f;
+            y += x[j] * f;
+        }
+        m = up;
+    }
+    if constexpr (PARTS > 1) {
+        tops[part0][which][lane] = m;
+        sums[part0][which][lane] = total;
+        outs[part0][which][lane] = y;
+        __syncthreads();
+        if (part0 > 0) return;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] += x[j][k] * f;
+        for (int i = 1; i < PARTS; ++i) m = fmaxf(m, tops[i][which][lane]);
+        total = 0.0f;
+        y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            const float of = tops[i][which][lane];
+            const float f = of == m || of == -kInf ? 1.0f : __builtin_amdgcn_exp2f(of - m);
+            total += sums[i][which][lane] * f;
+            y += outs[i][which][lane] * f;
         }
     }
+    if (!live) return;
     const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
     T* to = static_cast<T*>(a.out) + b * a.os[0] +
             (static_cast<int64_t>(g) * a.group + row - t * a.group) * a.os[1] + t * a.os[2] + d0;
@@ -588,24 +633,30 @@ __global__ __launch_bounds__(256) void attend4_join_kernel(const Attend4Args a, 
     *reinterpret_cast<Run4<T, 4>*>(to) = z;
 }
 
+template <typename T, int D, int PARTS>
+void launch_join(const Attend4Args& a, int64_t lines, hipStream_t st) {
+    const int per = 256 / (D / 4 * PARTS);
+    hipLaunchKernelGGL((attend4_join_kernel<T, D, PARTS>),
+                       dim3(static_cast<unsigned>((lines + per - 1) / per)), dim3(256), 0, st, a,
+                       static_cast<uint32_t>(lines));
+}
+
+template <typename T, int D, int WAVES>
+void launch_k(const Attend4Args& a, dim3 grid, hipStream_t st) {
+    hipLaunchKernelGGL((attend4_kernel<T, D, WAVES>), grid, dim3(64 * WAVES), 0, st, a);
+}
+
 template <typename T, int D>
 hipError_t launch_d(const Attend4Args& a, const Attend4Plan& p, int64_t heads, hipStream_t st) {
     const dim3 grid(static_cast<unsigned>(heads * p.row_groups * p.splits));
-    if (p.waves == 8)
-        hipLaunchKernelGGL((attend4_kernel<T, D, 8, 1>), grid, dim3(512), 0, st, a);
-    else if (p.row_waves == 1)
-        hipLaunchKernelGGL((attend4_kernel<T, D, 4, 1>), grid, dim3(256), 0, st, a);
-    else if (p.row_waves == 2)
-        hipLaunchKernelGGL((attend4_kernel<T, D, 4, 2>), grid, dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((attend4_kernel<T, D, 4, 4>), grid, dim3(256), 0, st, a);
-    if (p.splits > 1) {
-        const int64_t lines = heads * p.rows;
-        const int per = 256 / (D / 4);
-        hipLaunchKernelGGL((attend4_join_kernel<T, D>),
-                           dim3(static_cast<unsigned>((lines + per - 1) / per)), dim3(256), 0, st,
-                           a, static_cast<uint32_t>(lines));
+    switch (p.waves) {
+        case 1: launch_k<T, D, 1>(a, grid, st); break;
+        case 2: launch_k<T, D, 2>(a, grid, st); break;
+        case 4: launch_k<T, D, 4>(a, grid, st); break;
+        default: launch_k<T, D, 8>(a, grid, st); break;
     }
+    if (p.splits > 8) launch_join<T, D, 8>(a, heads * p.rows, st);
+    else if (p.splits > 1) launch_join<T, D, 1>(a, heads * p.rows, st);
     return hipGetLastError();
 }
 

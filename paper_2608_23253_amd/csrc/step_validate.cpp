@@ -144,15 +144,15 @@ Attend4Plan attend4_plan(const e2s_cache4& c, const e2s_cache4_attend_shape& s) 
     Attend4Plan p{};
     const int64_t B = s.batch, G = c.num_kv_heads, D = c.head_dim;
     p.rows = static_cast<int64_t>(s.num_heads) / G * s.num_queries;
-    p.row_waves = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : 4;
-    p.row_groups = (p.rows + 16 * p.row_waves - 1) / (16 * p.row_waves);
+    p.row_groups = (p.rows + 15) / 16;
     const int64_t units = B * G * p.row_groups;
-    p.waves = p.row_waves == 1 && units < 256 && s.max_tokens <= 2048 ? 8 : 4;
-    const int64_t unit = static_cast<int64_t>(kStep4) * (p.waves / p.row_waves);
-    // Keys are split until 1024 workgroups fill the device.
-    int64_t per = (s.max_tokens * units + 1023) / 1024;
-    if (p.waves == 8) per = s.max_tokens;
-    p.chunk = std::max<int64_t>(1, (per + unit - 1) / unit) * unit;
+    if (units < 256 && s.max_tokens <= 2048) p.waves = 8;
+    else p.waves = units < 512 ? 4 : units < 2048 ? 2 : 1;
+    const int64_t unit = static_cast<int64_t>(kStep4) * p.waves;
+    int64_t per = s.max_tokens;
+    const int64_t waves = p.waves == 2 ? 4096 : 3072;
+    if (p.waves == 2 || p.waves == 4) per = (s.max_tokens * units * p.waves + waves - 1) / waves;
+    p.chunk = (per + unit - 1) / unit * unit;
     p.splits = (s.max_tokens + p.chunk - 1) / p.chunk;
     const size_t all = static_cast<size_t>(B * G * p.rows);
     size_t at = 0;

@@ -26,10 +26,9 @@ constexpr int kStep4 = 128;          // keys of a wave's step
 // How an attention call is cut into workgroups, from its sizes alone.
 struct Attend4Plan {
     int64_t rows;        // query rows of one key head: H/Hkv * T, row = t * (H/Hkv) + head
-    int waves;           // of a workgroup: 4 or 8
-    int row_waves;       // of them along the rows, 16 each: 1, 2 or 4; the others part the keys
-    int64_t row_groups;  // workgroups along the rows
-    int64_t chunk;       // keys of a workgroup, a multiple of kStep4 * waves / row_waves
+    int64_t row_groups;  // workgroups along the rows, 16 each
+    int waves;           // of a workgroup, which part its keys: 1, 2, 4 or 8
+    int64_t chunk;       // keys of a workgroup, a multiple of kStep4 * waves
     int64_t splits;      // workgroups along the keys at max_tokens
     size_t max_off, sum_off, part_off, bytes;    // workspace regions
 };

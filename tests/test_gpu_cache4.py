@@ -316,3 +316,31 @@ def test_strided_pools():
     H.same_tables(pool, [kk[:, 1].cpu().numpy(), ks.cpu().numpy(), vv[:, 1].cpu().numpy(),
                          vs.float().cpu().numpy()], None)
     assert not kk[:, 0].any() and not kk[:, 2].any() and not vv[:, 0].any() and not vv[:, 2].any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("B,G,T,most", [(64, 32, 1, 90), (70, 8, 1, 300), (3, 4, 2, 5000)])
+def test_every_split(kind, B, G, T, most):
+    """One, two and four waves that part the keys, several workgroups to a sequence; sequences
+    read the same pages."""
+    rng = np.random.default_rng(16)
+    d, P = 64, 32
+    one = min(most, 320)
+    pool, table = H.filled(rng, 1, G, P, d, [one])
+    pages = np.array([[table[0][i % (one // P)] for i in range(-(-most // P))]] * B, np.int32)
+    lengths = [int(x) for x in rng.integers(0, most + 1, B)]
+    lengths[0] = most
+    some = [0, 1, B - 1]                               # compared with float64
+    q = torch.from_numpy(rng.standard_normal((B, G, T, d)))
+    qd = device(q, kind)
+    out = E.cache4_attend(qd, cache_of(pool), ints(pages), ints(lengths))
+    ref, tol = H.attend(pool, pages[some], [lengths[b] for b in some], qd.double().cpu()[some],
+                        kind)
+    check(out[some], ref, tol)
+    # and the others with calls of one sequence
+    for b in range(2, B - 1, 17):
+        alone = E.cache4_attend(qd[b:b + 1], cache_of(pool), ints(pages[b:b + 1]),
+                                ints(lengths[b:b + 1]))
+        r2, t2 = H.attend(pool, pages[b:b + 1], lengths[b:b + 1], qd.double().cpu()[b:b + 1], kind)
+        check(alone, r2, t2)
+        check(out[b:b + 1], r2, t2)
