@@ -89,13 +89,14 @@ def _weight(w, name, x, D):
     return w.data_ptr()
 
 
-def _weight_code(q_weight, k_weight, x):
+def _weight_code(q_weight, k_weight, code):
     """The weights' one dtype."""
-    torch = _torch()
-    kinds = {w.dtype for w in (q_weight, k_weight) if w is not None}
-    if len(kinds) > 1:
+    w = k_weight if q_weight is None else q_weight
+    if w is None:
+        return code
+    if k_weight is not None and k_weight.dtype is not w.dtype:
         raise TypeError("q_weight and k_weight must be of one type")
-    return 0 if kinds == {torch.float32} else _dtype_code(x)
+    return 0 if w.dtype is _torch().float32 else code
 
 
 def _positions(positions, plan, B, T):
@@ -117,52 +118,146 @@ def _positions(positions, plan, B, T):
 _NONE = (0, 0, 0)
 
 
-def _rows_of(t, name, x, D):
-    """The strides of a [B, heads, T, d] tensor beside x's; its number of heads."""
-    st = _rows(t, name, x.dtype)
-    shape = t.shape
-    if shape[0] != x.shape[0] or shape[2] != x.shape[2] or shape[3] != D:
-        raise ValueError(f"{name} {tuple(shape)} must be [B, heads, T, {D}] with one B and T")
-    return st[:3], shape[1]
-
-
 def _made_like(t, stream):
-    """An output beside t, its rows contiguous."""
+    """An output beside t, its rows contiguous, and its strides."""
     torch = _torch()
     o = _like(t, stream) if stream is not None else torch.empty_like(t)
-    if o.stride(3) != 1:                 # rows one element apart: torch may order them first
+    st = o.stride()
+    if st[3] != 1:                       # rows one element apart: torch may order them first
         o = _like(t, stream, torch.contiguous_format)
-    return o
+        st = o.stride()
+    return o, st[:3]
+
+
+def _inputs(q, k, positions, plan, q_weight, k_weight, eps):
+    """The checked inputs of a call: the head of its record, q's and k's strides, those of the
+    positions, and the weights' addresses."""
+    x = q if q is not None else k
+    D = plan.head_dim
+    heads, strides = [], []
+    for t, name in ((q, "q"), (k, "k")):
+        if t is None:
+            heads.append(0)
+            strides += _NONE
+            continue
+        strides += _rows(t, name, x.dtype)[:3]
+        shape = t.shape
+        if shape[0] != x.shape[0] or shape[2] != x.shape[2] or shape[3] != D:
+            raise ValueError(f"{name} {tuple(shape)} must be [B, heads, T, {D}] with one B and T")
+        heads.append(shape[1])
+    B, T = x.shape[0], x.shape[2]
+    ps = _positions(positions, plan, B, T)
+    weights = _weight(q_weight, "q_weight", x, D), _weight(k_weight, "k_weight", x, D)
+    code = _dtype_code(x)
+    return ((B, T, *heads, code, _weight_code(q_weight, k_weight, code), eps, 0), strides, ps,
+            weights)
+
+
+def _forward(inputs, q, k, positions, plan, q_weight, k_weight, q_out, k_out, stream):
+    head, strides, ps, weights = inputs
+    out_strides, outs = [], []
+    for i, (t, name, o) in enumerate(((q, "q", q_out), (k, "k", k_out))):
+        if t is None:
+            if o is not None:
+                raise ValueError(f"{name}_out without {name}")
+            out_strides += _NONE
+        elif o is None:
+            o, st = _made_like(t, stream)
+            out_strides += st
+        else:
+            st = _rows(o, name + "_out", t.dtype)[:3]
+            if o.shape != t.shape:
+                raise ValueError(f"{name}_out must have {name}'s shape")
+            if o.data_ptr() == t.data_ptr() and list(st) != strides[3 * i:3 * i + 3]:
+                raise ValueError(f"{name}_out in the place of {name} must have its strides")
+            out_strides += st
+        outs.append(o)
+    if head[0] > 0 and head[1] > 0:
+        sh = _NORM.pack(*head, *strides, *_NONE, *_NONE, *out_strides, *ps)
+        _launch("e2s_norm_rotate", (q, k, positions, q_weight, k_weight, *outs),
+                _LIB.e2s_norm_rotate, sh, ctypes.byref(plan), positions.data_ptr(), _ptr(q),
+                _ptr(k), *weights, _ptr(outs[0]), _ptr(outs[1]), stream=stream)
+    return outs[0], outs[1]
+
+
+def _backward(inputs, q_grad, k_grad, q, k, positions, plan, q_weight, k_weight, want, stream):
+    """want: which weights' gradients."""
+    torch = _torch()
+    head, strides, ps, weights = inputs
+    B, T = head[:2]
+    grad_strides, out_strides, outs = [], [], []
+    for t, g, name in ((q, q_grad, "q"), (k, k_grad, "k")):
+        if t is None:
+            grad_strides += _NONE
+            out_strides += _NONE
+            outs.append(None)
+            continue
+        grad_strides += _rows(g, name + "_grad", t.dtype)[:3]
+        if g.shape != t.shape:
+            raise ValueError(f"{name}_grad must have {name}'s shape")
+        o, st = _made_like(t, stream)
+        out_strides += st
+        outs.append(o)
+    x = q if q is not None else k
+    dqw = dkw = work = None
+    size = 0
+    if want[0] or want[1]:
+        with _allocating_on(stream, x.device):
+            make = torch.empty_like if B > 0 and T > 0 else torch.zeros_like
+            dqw = make(q_weight) if want[0] else None
+            dkw = make(k_weight) if want[1] else None
+    if B > 0 and T > 0:
+        sh = _NORM.pack(*head, *strides, *grad_strides, *out_strides, *ps)
+        plan_ref = ctypes.byref(plan)
+        if want[0] or want[1]:
+            n = ctypes.c_size_t(0)
+            _raise(_LIB.e2s_norm_rotate_backward_workspace_size(sh, plan_ref, 1, ctypes.byref(n)),
+                   "e2s_norm_rotate_backward_workspace_size")
+            size = n.value
+            with _allocating_on(stream, x.device):
+                work = torch.empty(size, device=x.device, dtype=torch.uint8)
+        _launch("e2s_norm_rotate_backward",
+                (q, k, positions, q_weight, k_weight, q_grad, k_grad, *outs, dqw, dkw, work),
+                _LIB.e2s_norm_rotate_backward, sh, plan_ref, positions.data_ptr(), _ptr(q),
+                _ptr(k), *weights, _ptr(q_grad), _ptr(k_grad), _ptr(outs[0]), _ptr(outs[1]),
+                _ptr(dqw), _ptr(dkw), _ptr(work), size, stream=stream)
+    return outs[0], outs[1], dqw, dkw
 
 
 class _NormRotate(_Function):
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, positions, plan, eps):
+        inputs = _inputs(q, k, positions, plan, q_weight, k_weight, eps)
         ctx.save_for_backward(q, k, q_weight, k_weight, positions)
-        ctx.plan, ctx.eps = plan, eps
+        ctx.plan, ctx.inputs = plan, inputs
         ctx.set_materialize_grads(False)
-        return norm_rotate(q, k, positions, plan, q_weight, k_weight, eps)
+        return _forward(inputs, q, k, positions, plan, q_weight, k_weight, None, None, None)
 
     @staticmethod
-    def backward(ctx, *grads):
-        torch = _torch()
-        if torch.is_grad_enabled():
+    def backward(ctx, q_grad, k_grad):
+        if _torch().is_grad_enabled():
             raise RuntimeError("norm_rotate has no second derivative: take its gradients "
                                "without create_graph")
-        q, k, q_weight, k_weight, positions = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        want = [(need[0] or need[2]) and grads[0] is not None,
-                (need[1] or need[3]) and grads[1] is not None]
-        if not any(want):
+        need_q, need_k, need_qw, need_kw = ctx.needs_input_grad[:4]
+        if not (need_q or need_qw):
+            q_grad = None
+        if not (need_k or need_kw):
+            k_grad = None
+        if q_grad is None and k_grad is None:
             return (None,) * 7
+        q, k, q_weight, k_weight, positions = ctx.saved_tensors
+        inputs = ctx.inputs
+        if q_grad is None or k_grad is None:         # (of a tensor that has none: without it)
+            q, k = (t if g is not None else None for t, g in ((q, q_grad), (k, k_grad)))
+            inputs = _inputs(q, k, positions, ctx.plan, q_weight, k_weight, inputs[0][6])
         # (a broadcast gradient has no contiguous rows)
-        gq, gk = (g if not w or g.stride(3) == 1 or g.shape[3] == 1 else
-                  g.clone(memory_format=torch.contiguous_format) for g, w in zip(grads, want))
-        dq, dk, dqw, dkw = norm_rotate_backward(
-            gq if want[0] else None, gk if want[1] else None, q if want[0] else None,
-            k if want[1] else None, positions, ctx.plan, q_weight, k_weight, ctx.eps,
-            want_q_weight=need[2] and want[0], want_k_weight=need[3] and want[1])
-        return (dq if need[0] else None, dk if need[1] else None, dqw, dkw, None, None, None)
+        q_grad, k_grad = (g if g is None or g.stride(3) == 1 or g.shape[3] == 1 else
+                          g.clone(memory_format=_torch().contiguous_format)
+                          for g in (q_grad, k_grad))
+        dq, dk, dqw, dkw = _backward(inputs, q_grad, k_grad, q, k, positions, ctx.plan, q_weight,
+                                     k_weight, (need_qw and q is not None,
+                                                need_kw and k is not None), None)
+        return (dq if need_q else None, dk if need_k else None, dqw, dkw, None, None, None)
 
 
 def norm_rotate(q, k, positions, plan: RotaryPlan, q_weight=None, k_weight=None,
@@ -171,121 +266,42 @@ def norm_rotate(q, k, positions, plan: RotaryPlan, q_weight=None, k_weight=None,
     rows), every row divided by its root mean square (eps within the root), times its
     tensor's weight ([d], of the rows' type or float32, or None), and turned by `positions`
     as rotate_positions does (e2s_norm_rotate).  Returns (q_out, k_out); an output may be its
-    input.  Outputs that are not given have a gradient where q, k or a weight asks for one."""
+    input.  Outputs that are not given have a gradient where q, k or a weight asks for one
+    (a first one: its own gradient is an error)."""
     torch = _torch()
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
-    if torch.is_grad_enabled() and any(
-            isinstance(t, torch.Tensor) and t.requires_grad for t in (q, k, q_weight, k_weight)):
+    if torch.is_grad_enabled() and (x.requires_grad or (k is not None and k.requires_grad) or
+                                    (q_weight is not None and q_weight.requires_grad) or
+                                    (k_weight is not None and k_weight.requires_grad)):
         if q_out is not None or k_out is not None:
             raise ValueError("an output that is given has no gradient: give none, or call "
                              "under torch.no_grad()")
         with _allocating_on(stream, x.device):
             return _NormRotate.apply(q, k, q_weight, k_weight, positions, plan, eps)
-    D = plan.head_dim
-    _rows(x, "q" if q is not None else "k")
-    heads, strides, out_strides, ptrs, outs = [], [], [], [], []
-    for t, name, o in ((q, "q", q_out), (k, "k", k_out)):
-        if t is None:
-            if o is not None:
-                raise ValueError(f"{name}_out without {name}")
-            heads.append(0)
-            strides += _NONE
-            out_strides += _NONE
-            ptrs += (None, None)
-            outs.append(None)
-            continue
-        st, h = _rows_of(t, name, x, D)
-        if o is None:
-            o = _made_like(t, stream)
-            so = o.stride()[:3]
-        else:
-            so = _rows(o, name + "_out", x.dtype)[:3]
-            if o.shape != t.shape:
-                raise ValueError(f"{name}_out must have {name}'s shape")
-            if o.data_ptr() == t.data_ptr() and so != st:
-                raise ValueError(f"{name}_out in the place of {name} must have its strides")
-        heads.append(h)
-        strides += st
-        out_strides += so
-        ptrs += (t.data_ptr(), o.data_ptr())
-        outs.append(o)
-    B, T = x.shape[0], x.shape[2]
-    ps = _positions(positions, plan, B, T)
-    qw, kw = _weight(q_weight, "q_weight", x, D), _weight(k_weight, "k_weight", x, D)
-    if B > 0 and T > 0:
-        sh = _NORM.pack(B, T, *heads, _dtype_code(x), _weight_code(q_weight, k_weight, x), eps, 0,
-                        *strides, *_NONE, *_NONE, *out_strides, *ps)
-        _launch("e2s_norm_rotate", (q, k, positions, q_weight, k_weight, *outs),
-                _LIB.e2s_norm_rotate, sh, ctypes.byref(plan), positions.data_ptr(), ptrs[0],
-                ptrs[2], qw, kw, ptrs[1], ptrs[3], stream=stream)
-    return outs[0], outs[1]
+    inputs = _inputs(q, k, positions, plan, q_weight, k_weight, eps)
+    return _forward(inputs, q, k, positions, plan, q_weight, k_weight, q_out, k_out, stream)
 
 
 def norm_rotate_backward(q_grad, k_grad, q, k, positions, plan: RotaryPlan, q_weight=None,
-                         k_weight=None, eps: float = 1e-6, want_q_weight: Optional[bool] = None,
-                         want_k_weight: Optional[bool] = None, stream: Optional[int] = None):
+                         k_weight=None, eps: float = 1e-6, want_q_weight: bool = True,
+                         want_k_weight: bool = True, stream: Optional[int] = None):
     """The gradients of norm_rotate's inputs from those of its outputs
     (e2s_norm_rotate_backward): (q's, k's, q_weight's, k_weight's), None for a tensor or weight
-    that is None.  want_q_weight, want_k_weight: False leaves that weight's out.  It keeps no
-    state, so it may be captured in a graph by itself; autograd calls it."""
-    torch = _torch()
-    x = q if q is not None else k
-    if x is None:
+    that is None, and for the weight of a tensor that is.  want_q_weight, want_k_weight: False
+    leaves that weight's out.  It keeps no state, so it may be captured in a graph by itself;
+    autograd calls it."""
+    if q is None and k is None:
         raise ValueError("q or k is needed")
-    D = plan.head_dim
-    _rows(x, "q" if q is not None else "k")
-    heads, strides, grad_strides, out_strides, ptrs, outs = [], [], [], [], [], []
     for t, g, name in ((q, q_grad, "q"), (k, k_grad, "k")):
         if (t is None) != (g is None):
             raise ValueError(f"{name} and {name}_grad go together")
-        if t is None:
-            heads.append(0)
-            strides += _NONE
-            grad_strides += _NONE
-            out_strides += _NONE
-            ptrs.append((None, None, None))
-            outs.append(None)
-            continue
-        st, h = _rows_of(t, name, x, D)
-        if g.shape != t.shape:
-            raise ValueError(f"{name}_grad must have {name}'s shape")
-        o = _made_like(t, stream)
-        heads.append(h)
-        strides += st
-        grad_strides += _rows(g, name + "_grad", x.dtype)[:3]
-        out_strides += o.stride()[:3]
-        ptrs.append((t.data_ptr(), g.data_ptr(), o.data_ptr()))
-        outs.append(o)
-    B, T = x.shape[0], x.shape[2]
-    ps = _positions(positions, plan, B, T)
-    qw, kw = _weight(q_weight, "q_weight", x, D), _weight(k_weight, "k_weight", x, D)
-    # (a weight without its tensor has no gradient)
-    want = [w is not None and t is not None and ask is not False
-            for w, t, ask in ((q_weight, q, want_q_weight), (k_weight, k, want_k_weight))]
-    with _allocating_on(stream, x.device):
-        dqw, dkw = (torch.zeros_like(w) if ask and (B == 0 or T == 0) else
-                    torch.empty_like(w) if ask else None
-                    for w, ask in zip((q_weight, k_weight), want))
-    if B > 0 and T > 0:
-        sh = _NORM.pack(B, T, *heads, _dtype_code(x), _weight_code(q_weight, k_weight, x), eps, 0,
-                        *strides, *grad_strides, *out_strides, *ps)
-        work, size = None, 0
-        if any(want):
-            n = ctypes.c_size_t(0)
-            _raise(_LIB.e2s_norm_rotate_backward_workspace_size(sh, ctypes.byref(plan), 1,
-                                                                ctypes.byref(n)),
-                   "e2s_norm_rotate_backward_workspace_size")
-            size = int(n.value)
-            with _allocating_on(stream, x.device):
-                work = torch.empty(size, device=x.device, dtype=torch.uint8)
-        _launch("e2s_norm_rotate_backward",
-                (q, k, positions, q_weight, k_weight, q_grad, k_grad, *outs, dqw, dkw, work),
-                _LIB.e2s_norm_rotate_backward, sh, ctypes.byref(plan), positions.data_ptr(),
-                ptrs[0][0], ptrs[1][0], qw, kw, ptrs[0][1], ptrs[1][1], ptrs[0][2], ptrs[1][2],
-                _ptr(dqw), _ptr(dkw), _ptr(work), size, stream=stream)
-    return outs[0], outs[1], dqw, dkw
+    inputs = _inputs(q, k, positions, plan, q_weight, k_weight, eps)
+    want = (q_weight is not None and q is not None and want_q_weight,
+            k_weight is not None and k is not None and want_k_weight)
+    return _backward(inputs, q_grad, k_grad, q, k, positions, plan, q_weight, k_weight, want,
+                     stream)
 
 
 # ---------------------------------------------------------------------------
