@@ -110,8 +110,8 @@ typedef struct {
     void* v_scale;          /* [num_pages, Hkv, P] bfloat16, 16-byte aligned          */
 } e2s_cache4;
 
-/* New tokens into the cache, by the rules of e2s_cache_append (k, v, pages, start, count_opt
- * and src_idx_opt as there).  A token's codes and scales do not depend on other tokens; no
+/* New tokens into the cache, by e2s_cache_append's rules for k, v, pages, start, count_opt and
+ * src_idx_opt.  A token's codes and scales do not depend on other tokens; no
  * other token of a page changes.  Two calls that write tokens of one page are ordered by
  * the caller (neighbouring tokens share bytes). */
 E2S_API e2s_status e2s_cache4_append(const e2s_cache4* cache, const e2s_cache_append_shape* shape,

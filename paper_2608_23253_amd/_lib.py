@@ -152,10 +152,10 @@ def lib() -> ctypes.CDLL:
 
 
 def header_entry_points(path: str = HEADER) -> list:
-    """Names of the functions include/e2s.h declares."""
+    """Names of the functions a header of the library (include/e2s.h) declares."""
     with open(path) as f:
         text = f.read()
-    return sorted(set(re.findall(r"\b(e2s_[a-z_]+)\s*\(", text)))
+    return sorted(set(re.findall(r"\b(e2s_[a-z0-9_]+)\s*\(", text)))
 
 
 # ---------------------------------------------------------------------------

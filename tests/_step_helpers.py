@@ -179,7 +179,7 @@ class Pool4:
         return out
 
 
-def same_tables(pool, got, ref_written):
+def same_tables(pool, got):
     """The tables `got` (k, ks, v, vs numpy, vs float32) hold what the pool does: the same
     scales everywhere, and the same bytes but for codes under a NaN scale."""
     k, ks, v, vs = got
@@ -193,8 +193,6 @@ def same_tables(pool, got, ref_written):
     one = (~np.isnan(pool.vs)).reshape(p, G, -1, 1, 16, 2).astype(np.uint8)
     mask = one[..., 0] * 15 + one[..., 1] * 240
     assert np.array_equal(v & mask, pool.v & mask)
-    if ref_written is not None:                          # rows that nothing wrote
-        assert np.array_equal(k[~ref_written], pool.k[~ref_written])
 
 
 # Terms of 4 bits on a scale that takes the largest to 1.93 .. 3.88, each the last one's residual

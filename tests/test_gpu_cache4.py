@@ -86,7 +86,7 @@ def test_append_holds_what_is_documented(case):
     k64, v64 = kd.double().cpu().numpy(), vd.double().cpu().numpy()
     for b in range(B):
         pool2.append(list(wide[b]), starts[b], k64[b][:, :n[b]], v64[b][:, :n[b]])
-    H.same_tables(pool2, tables_of(cache), None)
+    H.same_tables(pool2, tables_of(cache))
     got = E.cache4_read(cache, ints(wide), ints(starts), T,
                         count=None if counts is None else ints(counts), dtype=torch.float32)
     for b in range(B):
@@ -118,7 +118,7 @@ def test_append_what_the_pruner_kept():
     src = np.where((idx < 0) | (idx >= 30), 30, idx)
     for b in range(2):
         pool.append(list(wide[b]), [40, 0][b], kz[b][:, src[b]], vz[b][:, src[b]])
-    H.same_tables(pool, tables_of(cache), None)
+    H.same_tables(pool, tables_of(cache))
 
 
 def test_values_that_are_not_finite_take_their_block_or_row():
@@ -131,7 +131,7 @@ def test_values_that_are_not_finite_take_their_block_or_row():
     table = np.array([[1]], np.int32)
     E.cache4_append(cache, ints(table), ints([30]), k.cuda(), v.cuda())
     pool.append([1], 30, k[0].double().numpy(), v[0].double().numpy())
-    H.same_tables(pool, tables_of(cache), None)
+    H.same_tables(pool, tables_of(cache))
     gk, gv = E.cache4_read(cache, ints(table), ints([30]), 2, dtype=torch.float32)
     assert torch.isnan(gk[0, 0, 1, 32:64]).all() and torch.isnan(gk).sum() == 32
     assert not torch.isnan(gv).any()
@@ -314,7 +314,7 @@ def test_strided_pools():
     E.cache4_append(cache, ints(table), ints([70]), new.cuda(), new.cuda())
     pool.append(list(table[0]), 70, new[0].double().numpy(), new[0].double().numpy())
     H.same_tables(pool, [kk[:, 1].cpu().numpy(), ks.cpu().numpy(), vv[:, 1].cpu().numpy(),
-                         vs.float().cpu().numpy()], None)
+                         vs.float().cpu().numpy()])
     assert not kk[:, 0].any() and not kk[:, 2].any() and not vv[:, 0].any() and not vv[:, 2].any()
 
 

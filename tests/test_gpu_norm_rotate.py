@@ -115,7 +115,7 @@ def test_backward_is_the_forward_passes_derivative():
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_no_weight_at_identity_is_the_rotation_of_unit_rows(kind):
-    """Rows whose mean square is 1 - eps exactly keep their values: +-1 rows, eps 2^-20."""
+    """Rows of +-1, whose mean square is 1 (an eps of 2^-40 is lost beside it), keep their values."""
     dtype = H.DTYPES[kind]
     g = torch.Generator().manual_seed(5)
     x = torch.randint(0, 2, (2, 3, 9, 64), generator=g).mul(2).sub(1).to(dtype).cuda()
