@@ -7,6 +7,11 @@
 // both maxima are a few DPP steps, and every element is read once.  Key codes are written from
 // the lanes that hold them.  Value bytes hold two tokens of one dimension, so value codes
 // cross LDS once, and what other tokens of the group hold is merged in.
+//
+// 128 kept tokens of 64 x 576, 32 heads, bf16 (134 MB picked by an index, 18 MB written): 39 us,
+// 3.9 TB/s; 48 with maxima and value codes an element at a time, 22 instructions to an
+// element (the vector unit was busy for 45 of them); workgroups of 128 or 512 threads: 50 and 55.
+// Read back (134 MB written): 28 us, 5.5 TB/s.  One token of 64 sequences: 4.0 and 3.5 us, the launch.
 #include "serve_device.h"
 #include "step_kernels.h"
 
@@ -34,6 +39,35 @@ struct Append4Args {
     int64_t ss[2][3];                // sequence, head, token, in elements
     int T, N, groups;
 };
+
+// The largest magnitude of a packet, an infinity if one of them is or is NaN.  Magnitudes are
+// ordered as their bits are, and what is not finite comes last.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t top_half(const u32x4& a) {
+    u16x2 m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = __builtin_bit_cast(u16x2, a[i] & 0x7FFF7FFFu);
+    const u16x2 t = __builtin_elementwise_max(__builtin_elementwise_max(m[0], m[1]),
+                                              __builtin_elementwise_max(m[2], m[3]));
+    return max(static_cast<uint32_t>(t.x), static_cast<uint32_t>(t.y));
+}
+__device__ __forceinline__ float packet_top(const Packet<uint16_t>& p) {
+    const uint32_t m = top_half(p.a);
+    return m < 0x7F80u ? __uint_as_float(m << 16) : kInf;
+}
+__device__ __forceinline__ float packet_top(const Packet<_Float16>& p) {
+    const uint32_t m = top_half(p.a);
+    return m < 0x7C00u ? f16lo(m) : kInf;
+}
+__device__ __forceinline__ float packet_top(const Packet<float>& p) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m = max(m, __float_as_uint(p.a[i]) & 0x7FFFFFFFu);
+        m = max(m, __float_as_uint(p.b[i]) & 0x7FFFFFFFu);
+    }
+    return m < 0x7F800000u ? __uint_as_float(m) : kInf;
+}
 
 __device__ __forceinline__ float quad_max(float v) {
     v = fmaxf(v, dpp<kQuadSwap1>(v));
@@ -70,6 +104,39 @@ __device__ __forceinline__ uint32_t value_code(float m, float s) {
     return (b2 ? 4u : 0u) | (b1 ? 2u : 0u) | (m > t * s ? 1u : 0u);
 }
 
+// The codes of 8 elements at a row's scale s, element 2 i in the low half of byte i.
+__device__ __forceinline__ uint32_t key_codes(const float (&e)[8], float s) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[0], e[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[2], e[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[4], e[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[6], e[7], s, 3);
+}
+// The conversion's scale is a power of two, so a value is divided by its own first.  A border
+// between codes has 11 bits (3 times the scale's 8), so an element of 8 or 11 bits that is not
+// one is 2^-11 of it away at least, and one that is comes out exactly, by a step of Newton's.
+// Elements of 24 bits are compared with the borders instead.
+template <typename T>
+__device__ __forceinline__ uint32_t value_codes(const float (&e)[8], float s) {
+    if constexpr (sizeof(T) == 4) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w |= (value_code(fabsf(e[i]), s) | (__float_as_uint(e[i]) >> 28 & 8u)) << (4 * i);
+        return w;
+    } else {
+        const float r = 1.0f / s;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float q = e[i] * r;
+            // (a negative zero keeps its sign)
+            y[i] = copysignf(__builtin_fmaf(__builtin_fmaf(-q, s, e[i]), r, q), e[i]);
+        }
+        return key_codes(y, 1.0f);
+    }
+}
+
 // The smallest bfloat16 s >= 2^-100 with amax <= 6 s, NaN for an infinite amax.  6 s is exact.
 __device__ __forceinline__ float value_scale(float amax) {
     uint32_t bits = __float_as_uint(amax / 6.0f) & 0xFFFF0000u;
@@ -84,7 +151,8 @@ __global__ __launch_bounds__(THREADS) void append4_kernel(const Append4Args a) {
     constexpr int kLanes = D / 8;                   // threads of a row
     constexpr int kRows = THREADS / kLanes;         // rows of a pass
     constexpr int kPad = D + 4;
-    __shared__ alignas(8) uint8_t codes[kGroup4 * kPad];     // of the values, a byte each
+    // of the values, a byte each: of 8 elements the even ones, then the odd ones
+    __shared__ alignas(8) uint8_t codes[kGroup4 * kPad];
     const uint32_t unit = blockIdx.x;
     const int g = static_cast<int>(unit % static_cast<uint32_t>(a.c.G));
     const uint32_t ub = unit / static_cast<uint32_t>(a.c.G);
@@ -104,8 +172,9 @@ __global__ __launch_bounds__(THREADS) void append4_kernel(const Append4Args a) {
     const int lane = threadIdx.x % kLanes, sub = threadIdx.x / kLanes;
     const Group4<D> at(a.c, page, g, static_cast<int>(first) & (a.c.P - 1));
 
-    // Values: thread (4 dimensions, 8 tokens) of `parts` owns 4 words of a word per dimension.
+    // Values: thread (4 dimensions, 8 tokens) owns a word of each dimension.
     constexpr int kParts = D, kPer = (kParts + THREADS - 1) / THREADS;
+    auto dim_of = [](int part, int j) { return (part >> 3) * 8 + (part >> 2 & 1) + 2 * j; };
     uint32_t mask[kPer], old[kPer][4];
 #pragma unroll
     for (int n = 0; n < kPer; ++n) {
@@ -116,7 +185,7 @@ __global__ __launch_bounds__(THREADS) void append4_kernel(const Append4Args a) {
         if (mask[n] != 0u && mask[n] != ~0u) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                old[n][j] = *reinterpret_cast<const uint32_t*>(at.v + ((part >> 2) * 4 + j) * 16 +
+                old[n][j] = *reinterpret_cast<const uint32_t*>(at.v + dim_of(part, j) * 16 +
                                                                (part & 3) * 4);
         }
     }
@@ -145,13 +214,7 @@ __global__ __launch_bounds__(THREADS) void append4_kernel(const Append4Args a) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             unpack(x[n][k], e[k]);
-            top[k] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float m = fabsf(e[k][i]);
-                top[k] = fmaxf(top[k], m < kInf ? m : kInf);      // (NaN too)
-            }
-            top[k] = quad_max(top[k]);
+            top[k] = quad_max(packet_top(x[n][k]));
         }
         top[1] = fmaxf(top[1], dpp<kRowHalfMirror>(top[1]));
         if (kLanes == 16) top[1] = fmaxf(top[1], dpp<kRowMirror>(top[1]));
@@ -163,24 +226,15 @@ __global__ __launch_bounds__(THREADS) void append4_kernel(const Append4Args a) {
         int ex = f <= 0.75f ? x2 - 3 : x2 - 2;
         if (top[0] == 0.0f || ex < kLowestScale) ex = kLowestScale;
         const float s = __builtin_ldexpf(1.0f, ex);
-        uint32_t w = 0;
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[0][0], e[0][1], s, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[0][2], e[0][3], s, 1);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[0][4], e[0][5], s, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, e[0][6], e[0][7], s, 3);
-        *reinterpret_cast<uint32_t*>(at.k + r * (D / 2) + lane * 4) = w;
+        *reinterpret_cast<uint32_t*>(at.k + r * (D / 2) + lane * 4) = key_codes(e[0], s);
         if ((lane & 3) == 0)
             at.k_scale[key_scale_at<D>(r, lane >> 2)] =
                 static_cast<uint8_t>(finite ? ex + 127 : 255);
         const float vs = value_scale(top[1]);
-        uint32_t c[2] = {0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            c[i >> 2] |= (value_code(fabsf(e[1][i]), vs) |
-                          (__float_as_uint(e[1][i]) >> 28 & 8u)) << (8 * (i & 3));
+        const uint32_t c = value_codes<T>(e[1], vs);
         uint32_t* to = reinterpret_cast<uint32_t*>(codes + r * kPad + lane * 8);
-        to[0] = c[0];
-        to[1] = c[1];
+        to[0] = c & 0x0F0F0F0Fu;
+        to[1] = c >> 4 & 0x0F0F0F0Fu;
         if (lane == 0) at.v_scale[r] = from_f32<uint16_t>(vs);
     }
     __syncthreads();
@@ -188,7 +242,7 @@ __global__ __launch_bounds__(THREADS) void append4_kernel(const Append4Args a) {
     for (int n = 0; n < kPer; ++n) {
         if (mask[n] == 0u) continue;
         const int part = threadIdx.x + n * THREADS, t8 = (part & 3) * 8, d4 = (part >> 2) * 4;
-        uint32_t y[4];                               // byte j: dimension d4 + j of two tokens
+        uint32_t y[4];                               // byte j: dimension dim_of(part, j), two tokens
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t* lo = reinterpret_cast<const uint32_t*>(codes + (t8 + 2 * i) * kPad + d4);
@@ -207,7 +261,7 @@ __global__ __launch_bounds__(THREADS) void append4_kernel(const Append4Args a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (mask[n] != ~0u) z[j] = (z[j] & mask[n]) | (old[n][j] & ~mask[n]);
-            *reinterpret_cast<uint32_t*>(at.v + (d4 + j) * 16 + (part & 3) * 4) = z[j];
+            *reinterpret_cast<uint32_t*>(at.v + dim_of(part, j) * 16 + (part & 3) * 4) = z[j];
         }
     }
 }

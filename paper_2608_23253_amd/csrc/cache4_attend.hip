@@ -23,9 +23,21 @@
 // the two halves of a key product's k take two terms of the query at once.
 //
 // One pass: a running maximum and sum per row; the maximum is raised (and the output rescaled)
-// only when a logit passes it by 2^8 in the exponential.  Waves take rows of 16, or part the
-// keys and merge in LDS; keys are split over workgroups where there are few rows, and
+// only when a logit passes it by 2^8 in the exponential.  16 rows to a workgroup, whose waves
+// part its keys and merge in LDS; keys are split over workgroups where there are few rows, and
 // attend4_join_kernel joins the parts.
+//
+// What bounds it: a decoding step reads 133 bytes per token and key head (d = 128, of 258 in 8
+// bits), of which 4 sequences of 60000 to 131072 keys take 35 us (4.8 TB/s) and 64 of 130 to
+// 1200 keys, 32 heads, f16, 48 us; with many rows the vector unit, some 410 instructions to a
+// step beside 40 matrix products (1300 cycles): 2 x 1024 queries of 2048 keys, 28 heads, bf16: 79
+// to 89 us, 510 to 570 TFLOP/s of the 45 GFLOP that the mask leaves.  Two waves to a SIMD (213
+// registers) hold a step's keys and values: three waves spilled (107 us for 91).  What the
+// steps of making it fast gave for the 1024 queries, in us: 155 as first written; 116 with two
+// waves to a SIMD; 102 with loops that leave keys and outputs in place; 91 with addresses from
+// one lookup a segment and maxima without the compiler's quieting; 89 with the values' loads
+// before the logits and the keys' after them.  Logits of the next step beside this one's weights
+// (245 registers) gave nothing: 103 for 102.
 #include <type_traits>
 
 #include "serve_device.h"

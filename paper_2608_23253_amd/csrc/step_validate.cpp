@@ -146,6 +146,15 @@ Attend4Plan attend4_plan(const e2s_cache4& c, const e2s_cache4_attend_shape& s) 
     p.rows = static_cast<int64_t>(s.num_heads) / G * s.num_queries;
     p.row_groups = (p.rows + 15) / 16;
     const int64_t units = B * G * p.row_groups;
+    // The device holds 2048 waves at two to a SIMD.  From as many units on, each is one wave, and
+    // nothing is joined (64 sequences of up to 1200 keys, 32 heads: 47 us; two waves 47, four 53).
+    // Fewer units part their keys, in workgroups of two or four waves, until 4096 or 3072 waves
+    // are there, more than fit, as lengths are mostly shorter than the longest: 1344 units (16
+    // sequences of up to 4200 keys, ragged counts) take 38 us so, 45 with 3072 waves, 52 with
+    // four waves to a workgroup; 16 units of up to 131072 keys 35 us with 3072, 37 with 2048, 44
+    // with 4096, and 43 in workgroups of two.  Short sequences of few units: one workgroup of
+    // eight waves has all keys (one of up to 1100 keys, 4 key heads: 8.0 us; in parts 6.0 and a
+    // join of 3.3).
     if (units < 256 && s.max_tokens <= 2048) p.waves = 8;
     else p.waves = units < 512 ? 4 : units < 2048 ? 2 : 1;
     const int64_t unit = static_cast<int64_t>(kStep4) * p.waves;

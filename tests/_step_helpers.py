@@ -197,8 +197,8 @@ def same_tables(pool, got):
 
 # Terms of 4 bits on a scale that takes the largest to 1.93 .. 3.88, each the last one's residual
 # on a scale 2^-4 of its: n terms hold 4 n bits, or, e4m3's smallest step being 2^-9, leave half
-# of 2^-9 2^-4(n - 1) of a largest that is near 2 at least: 2^-11 - 4 (n - 1) of it, and 4%.  n = 2, 3, 6
-# for queries, 3, 4, 6 for weights.
+# of 2^-9 2^-4(n - 1) of a largest that is near 2 at least: 2^-11 - 4 (n - 1) of it, and 4%.
+# n = 2, 3, 6 for queries, 3, 4, 6 for weights.
 Q_FLOOR = {"bf16": 1.04 * 2.0 ** -15, "f16": 1.04 * 2.0 ** -19, "f32": 1.04 * 2.0 ** -31}
 P_STEP = {"bf16": 2.0 ** -12, "f16": 2.0 ** -16, "f32": 2.0 ** -24}
 P_FLOOR = {"bf16": 1.04 * 2.0 ** -19, "f16": 1.04 * 2.0 ** -23, "f32": 1.04 * 2.0 ** -31}

@@ -344,3 +344,33 @@ def test_every_split(kind, B, G, T, most):
         r2, t2 = H.attend(pool, pages[b:b + 1], lengths[b:b + 1], qd.double().cpu()[b:b + 1], kind)
         check(alone, r2, t2)
         check(out[b:b + 1], r2, t2)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_value_codes_at_every_border(kind):
+    """Rows of every largest element's mantissa, beside the elements around each border between
+    codes: bf16 all that lie within 2^-6 of it, f16 the nearest on either side."""
+    dtype, d = H.DTYPES[kind], 64
+    rows = []
+    for m in range(128):
+        top = 1.0 + m / 128
+        s = H.value_scale(top)
+        near = []
+        for border in (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0):
+            x = torch.tensor(border * s, dtype=torch.float64).to(dtype)
+            for step in range(-4, 5):
+                near.append((x.view(torch.int16) + step).view(dtype).item())
+        for i in range(0, len(near), d - 1):
+            part = [min(v, top) for v in near[i:i + d - 1]]
+            rows.append([top] + part + [-0.0] * (d - 1 - len(part)))
+    v = torch.tensor(rows, dtype=torch.float64)
+    v = v * torch.where(torch.arange(d) % 2 == 1, -1.0, 1.0)
+    T = len(rows)
+    pages = -(-T // 128)
+    pool = H.Pool4(pages, 1, 128, d)
+    cache = cache_of(pool)
+    x = v[None, None].to(dtype)
+    assert torch.equal(x.double()[0, 0], v)
+    E.cache4_append(cache, ints([list(range(pages))]), ints([0]), x.cuda(), x.cuda())
+    pool.append(list(range(pages)), 0, v[None].numpy(), v[None].numpy())
+    H.same_tables(pool, tables_of(cache))
