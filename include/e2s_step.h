@@ -89,6 +89,8 @@ E2S_API e2s_status e2s_norm_rotate_backward(const e2s_norm_rotate_shape* shape,
  * A held element is its code's value times the scale; codes are to nearest, ties to the even
  * code.  A block (key) or row (value) that holds a NaN or an infinity has a NaN scale: all
  * of it is NaN.
+ *   Codes and scales that a caller writes itself are of these kinds: any code, exponent bytes 27
+ * to 252 and 0xFF, value scales of 2^-100 and more or NaN.
  *   Tokens lie in pages as those of the 8-bit cache do.  A page holds, for every key head:
  *   k        [P, d/2]: byte i of a token: elements 2i (low half) and 2i + 1
  *   k_scale  [P/16, 4, d/32, 4]: [n, r, c, u]: block c of token 16 n + 4 u + r
@@ -112,8 +114,9 @@ typedef struct {
 
 /* New tokens into the cache, by e2s_cache_append's rules for k, v, pages, start, count_opt and
  * src_idx_opt.  A token's codes and scales do not depend on other tokens; no
- * other token of a page changes.  Two calls that write tokens of one page are ordered by
- * the caller (neighbouring tokens share bytes). */
+ * other token of a page changes.  Neighbouring tokens share bytes: two calls that write
+ * tokens of one page are ordered by the caller, and no two sequences of a call write tokens of
+ * one page. */
 E2S_API e2s_status e2s_cache4_append(const e2s_cache4* cache, const e2s_cache_append_shape* shape,
                                      const int32_t* pages, const int32_t* start,
                                      const int32_t* count_opt, const int32_t* src_idx_opt,
