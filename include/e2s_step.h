@@ -90,7 +90,7 @@ E2S_API e2s_status e2s_norm_rotate_backward(const e2s_norm_rotate_shape* shape,
  * code.  A block (key) or row (value) that holds a NaN or an infinity has a NaN scale: all
  * of it is NaN.
  *   Codes and scales that a caller writes itself are of these kinds: any code, exponent bytes 27
- * to 252 and 0xFF, value scales of 2^-100 and more or NaN.
+ * to 253 and 0xFF, value scales of 2^-100 and more or NaN.
  *   Tokens lie in pages as those of the 8-bit cache do.  A page holds, for every key head:
  *   k        [P, d/2]: byte i of a token: elements 2i (low half) and 2i + 1
  *   k_scale  [P/16, 4, d/32, 4]: [n, r, c, u]: block c of token 16 n + 4 u + r
@@ -133,7 +133,8 @@ typedef struct {
 } e2s_cache4_read_shape;
 
 /* k_out, v_out [B, Hkv, T, d]: row j < count[b] of sequence b is the held key or value of
- * its token start[b] + j, rounded once to dtype (float32 holds it exactly); rows behind them
+ * its token start[b] + j, rounded once to dtype (float32 holds it exactly, up to its range;
+ * one past the range, which rounding up to a code can lead to, is an infinity); rows behind them
  * are left as they were.  A token before 0, past max_pages * P or whose page is outside
  * [0, num_pages) reads as zeros.  Base pointers and strides keep rows 16-byte aligned; either
  * output may be NULL. */

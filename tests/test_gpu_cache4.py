@@ -374,3 +374,37 @@ def test_value_codes_at_every_border(kind):
     E.cache4_append(cache, ints([list(range(pages))]), ints([0]), x.cuda(), x.cuda())
     pool.append(list(range(pages)), 0, v[None].numpy(), v[None].numpy())
     H.same_tables(pool, tables_of(cache))
+
+
+@pytest.mark.parametrize("d,P", [(64, 32), (128, 128)])
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+def test_every_magnitude_of_a_type(kind, d, P):
+    """Rows (and blocks of 32) anywhere in the type's range, from its smallest element to its
+    largest, held bit for bit; and a source row that several tokens name."""
+    dtype = H.DTYPES[kind]
+    info = torch.finfo(dtype)
+    rng = np.random.default_rng(17)
+    low = int(np.log2(info.tiny)) + int(np.log2(info.eps))
+    T, N = 200, 150
+    top = torch.from_numpy(rng.integers(low, int(np.log2(info.max)) + 1, (1, 1, N, d // 32, 1)))
+    x = torch.from_numpy(rng.uniform(1, 2, (1, 1, N, d // 32, 32))) * \
+        2.0 ** (top - torch.from_numpy(rng.integers(0, 5, (1, 1, N, d // 32, 32))))
+    x = (x * torch.from_numpy(rng.choice([-1.0, 1.0], x.shape))).reshape(1, 1, N, d)
+    x[0, 0, 0], x[0, 0, 1], x[0, 0, 2] = info.max, info.tiny * info.eps, 0
+    x[0, 0, 3, 1::2] = -info.max
+    x = x.clamp(-info.max, info.max).to(dtype)
+    idx = rng.integers(0, N, (1, T)).astype(np.int32)
+    idx[0, :4], idx[0, 50:60] = range(4), 7
+    pages = -(-(T + 5) // P)
+    pool = H.Pool4(pages, 1, P, d)
+    cache = cache_of(pool)
+    v = x.flip(2).contiguous()
+    E.cache4_append(cache, ints([list(range(pages))]), ints([5]), x.cuda(), v.cuda(),
+                    src_idx=ints(idx))
+    pool.append(list(range(pages)), 5, x[0][:, idx[0]].double().numpy(),
+                v[0][:, idx[0]].double().numpy())
+    H.same_tables(pool, tables_of(cache))
+    got = E.cache4_read(cache, ints([list(range(pages))]), ints([5]), T, dtype=torch.float32)
+    for which, y in zip("kv", got):
+        ref = torch.from_numpy(pool.rows(which, list(range(pages)), 5 + T, 0)[5:])
+        assert torch.equal(y[0, 0].cpu(), ref.float())
