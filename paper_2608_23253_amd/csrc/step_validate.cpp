@@ -11,6 +11,7 @@ namespace {
 constexpr double kBig = static_cast<double>(std::numeric_limits<int64_t>::max() / 16);
 constexpr int64_t kMaxStride = std::numeric_limits<int64_t>::max() / 64;
 constexpr double kItems = 4294967296.0;          // work-items of a launch
+constexpr int64_t kSimds = 1024;                 // 256 compute units of 4
 
 #define E2S_TRY_(expr)                         \
     do {                                       \
@@ -148,18 +149,18 @@ Attend4Plan attend4_plan(const e2s_cache4& c, const e2s_cache4_attend_shape& s) 
     const int64_t units = B * G * p.row_groups;
     // The device holds 2048 waves at two to a SIMD.  From as many units on, each is one wave, and
     // nothing is joined (64 sequences of up to 1200 keys, 32 heads: 47 us; two waves 47, four 53).
-    // Fewer units part their keys, in workgroups of two or four waves, until 4096 or 3072 waves
-    // are there, more than fit, as lengths are mostly shorter than the longest: 1344 units (16
-    // sequences of up to 4200 keys, ragged counts) take 38 us so, 45 with 3072 waves, 52 with
-    // four waves to a workgroup; 16 units of up to 131072 keys 35 us with 3072, 37 with 2048, 44
-    // with 4096, and 43 in workgroups of two.  Short sequences of few units: one workgroup of
-    // eight waves has all keys (one of up to 1100 keys, 4 key heads: 8.0 us; in parts 6.0 and a
+    // Fewer units part their keys, in workgroups of two or four waves, until four or three waves
+    // for each SIMD are there, more than fit, as lengths are mostly shorter than the longest: 1344
+    // units (16 sequences of up to 4200 keys, ragged counts) take 38 us with four, 45 with three,
+    // 52 with four waves to a workgroup; 16 units of up to 131072 keys 35 us with three, 37 with
+    // two, 44 with four, and 43 in workgroups of two.  Short sequences of few units: one workgroup
+    // of eight waves has all keys (one of up to 1100 keys, 4 key heads: 8.0 us; in parts 6.0 and a
     // join of 3.3).
     if (units < 256 && s.max_tokens <= 2048) p.waves = 8;
     else p.waves = units < 512 ? 4 : units < 2048 ? 2 : 1;
     const int64_t unit = static_cast<int64_t>(kStep4) * p.waves;
     int64_t per = s.max_tokens;
-    const int64_t waves = p.waves == 2 ? 4096 : 3072;
+    const int64_t waves = (p.waves == 2 ? 4 : 3) * kSimds;
     if (p.waves == 2 || p.waves == 4) per = (s.max_tokens * units * p.waves + waves - 1) / waves;
     p.chunk = (per + unit - 1) / unit * unit;
     p.splits = (s.max_tokens + p.chunk - 1) / p.chunk;
