@@ -224,12 +224,19 @@ def _backward(inputs, q_grad, k_grad, q, k, positions, plan, q_weight, k_weight,
     return outs[0], outs[1], dqw, dkw
 
 
+def _whole_rows(t):
+    """t, or a copy where its rows are not contiguous (a broadcast gradient's are not)."""
+    if t.stride(3) == 1 or t.shape[3] == 1:
+        return t
+    return t.clone(memory_format=_torch().contiguous_format)
+
+
 class _NormRotate(_Function):
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, positions, plan, eps):
         inputs = _inputs(q, k, positions, plan, q_weight, k_weight, eps)
         ctx.save_for_backward(q, k, q_weight, k_weight, positions)
-        ctx.plan, ctx.inputs = plan, inputs
+        ctx.plan, ctx.eps = plan, eps
         ctx.set_materialize_grads(False)
         return _forward(inputs, q, k, positions, plan, q_weight, k_weight, None, None, None)
 
@@ -245,15 +252,14 @@ class _NormRotate(_Function):
             k_grad = None
         if q_grad is None and k_grad is None:
             return (None,) * 7
+        # What is unpacked need not be what was saved: a hook gives copies, which have strides of
+        # their own, and a checkpoint makes tensors again.  So nothing that forward learned of
+        # their memory is used: the record is made, and checked, from the tensors in hand.
         q, k, q_weight, k_weight, positions = ctx.saved_tensors
-        inputs = ctx.inputs
-        if q_grad is None or k_grad is None:         # (of a tensor that has none: without it)
-            q, k = (t if g is not None else None for t, g in ((q, q_grad), (k, k_grad)))
-            inputs = _inputs(q, k, positions, ctx.plan, q_weight, k_weight, inputs[0][6])
-        # (a broadcast gradient has no contiguous rows)
-        q_grad, k_grad = (g if g is None or g.stride(3) == 1 or g.shape[3] == 1 else
-                          g.clone(memory_format=_torch().contiguous_format)
-                          for g in (q_grad, k_grad))
+        # (a tensor whose output has no gradient takes no part)
+        q, q_grad = (None, None) if q_grad is None else (_whole_rows(q), _whole_rows(q_grad))
+        k, k_grad = (None, None) if k_grad is None else (_whole_rows(k), _whole_rows(k_grad))
+        inputs = _inputs(q, k, positions, ctx.plan, q_weight, k_weight, ctx.eps)
         dq, dk, dqw, dkw = _backward(inputs, q_grad, k_grad, q, k, positions, ctx.plan, q_weight,
                                      k_weight, (need_qw and q is not None,
                                                 need_kw and k is not None), None)
