@@ -124,6 +124,20 @@ def _like(t, stream, order=None):
         return torch.empty_like(t, memory_format=order or torch.preserve_format)
 
 
+_AD = _lib._TORCH.autograd.forward_ad if _lib._TORCH is not None else None
+
+
+def _no_tangents(where, *tensors):
+    """Forward-mode differentiation has no rule here: an error says so where a launch, which
+    knows of values alone, would lose the tangents.  (Outside a dual level there are none: one
+    look, where torch says which level it is in.)"""
+    if getattr(_AD, "_current_level", 0) < 0:
+        return
+    for t in tensors:
+        if t is not None and _AD.unpack_dual(t).tangent is not None:
+            raise RuntimeError(f"{where} has no forward-mode derivative")
+
+
 def _rows(t, name, dtype=None):
     """The strides of a [B, H, T, d] tensor of rows: any, the last dimension contiguous."""
     if not (isinstance(t, _torch().Tensor) and t.is_cuda and t.dim() == 4 and
@@ -213,6 +227,7 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
+    _no_tangents("rotate_positions", q, k)
     if (x.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
         if q_out is not None or k_out is not None:
             raise ValueError("an output that is given has no gradient: give none, or call "
@@ -425,6 +440,7 @@ class CacheAttention:
         through the outputs is an error."""
         torch = _torch()
         qs = _rows(q, "q", self.dtype)
+        _no_tangents("attention over the 8-bit cache", q)
         if q.requires_grad and torch.is_grad_enabled():
             if out is not None:
                 raise ValueError("attention over the cache has no gradient for `out`: call it "

@@ -15,8 +15,8 @@ from typing import Optional
 
 from . import _lib
 from ._lib import _CURRENT_STREAM, _check, _dtype_code, _launch, _ptr, _raise, _torch
-from ._serve import (_I32, _I64, _P, RotaryPlan, _allocating_on, _Function, _like, _ref,
-                     _rows, _table, _vector)
+from ._serve import (_I32, _I64, _P, RotaryPlan, _allocating_on, _Function, _like, _no_tangents,
+                     _ref, _rows, _table, _vector)
 
 HEADER = os.path.join(os.path.dirname(_lib.PKG), "include", "e2s_step.h")
 
@@ -273,11 +273,13 @@ def norm_rotate(q, k, positions, plan: RotaryPlan, q_weight=None, k_weight=None,
     tensor's weight ([d], of the rows' type or float32, or None), and turned by `positions`
     as rotate_positions does (e2s_norm_rotate).  Returns (q_out, k_out); an output may be its
     input.  Outputs that are not given have a gradient where q, k or a weight asks for one
-    (a first one: its own gradient is an error)."""
+    (a first one: its own gradient is an error, as are tangents of forward-mode
+    differentiation)."""
     torch = _torch()
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k is needed")
+    _no_tangents("norm_rotate", q, k, q_weight, k_weight)
     if torch.is_grad_enabled() and (x.requires_grad or (k is not None and k.requires_grad) or
                                     (q_weight is not None and q_weight.requires_grad) or
                                     (k_weight is not None and k_weight.requires_grad)):
@@ -303,6 +305,7 @@ def norm_rotate_backward(q_grad, k_grad, q, k, positions, plan: RotaryPlan, q_we
     for t, g, name in ((q, q_grad, "q"), (k, k_grad, "k")):
         if (t is None) != (g is None):
             raise ValueError(f"{name} and {name}_grad go together")
+    _no_tangents("norm_rotate_backward", q_grad, k_grad, q, k, q_weight, k_weight)
     inputs = _inputs(q, k, positions, plan, q_weight, k_weight, eps)
     want = (q_weight is not None and q is not None and want_q_weight,
             k_weight is not None and k is not None and want_k_weight)
@@ -489,6 +492,7 @@ class Cache4Attention:
         `out` is not given and a backward pass through the output is an error."""
         torch = _torch()
         qs = _rows(q, "q", self.dtype)
+        _no_tangents("attention over the 4-bit cache", q)
         if q.requires_grad and torch.is_grad_enabled():
             if out is not None:
                 raise ValueError("attention over the cache has no gradient for `out`: call it "
