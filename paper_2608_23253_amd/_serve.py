@@ -149,6 +149,12 @@ def _rows(t, name, dtype=None):
     return st
 
 
+def _moved(shape, a, b):
+    """Whether rows of a shape lie elsewhere by strides b than by strides a (a dimension of one
+    may have any)."""
+    return a[:3] != b[:3] and any(n > 1 and x != y for n, x, y in zip(shape[:3], a, b))
+
+
 def _vector(t, name, n):
     """The address of an int32 [n] of per-sequence numbers."""
     torch = _torch()
@@ -261,7 +267,7 @@ def rotate_positions(q, k, positions, plan: RotaryPlan, inverse: bool = False, q
             so = _rows(o, name + "_out", dtype)
             if o.shape != shape:
                 raise ValueError(f"{name}_out must have {name}'s shape")
-            if o.data_ptr() == t.data_ptr() and so != st:
+            if o.data_ptr() == t.data_ptr() and _moved(shape, st, so):
                 raise ValueError(f"{name}_out in the place of {name} must have its strides")
         heads.append(shape[1])
         strides += st[:3]

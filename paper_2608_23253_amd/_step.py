@@ -15,8 +15,8 @@ from typing import Optional
 
 from . import _lib
 from ._lib import _CURRENT_STREAM, _check, _dtype_code, _launch, _ptr, _raise, _torch
-from ._serve import (_I32, _I64, _P, RotaryPlan, _allocating_on, _Function, _like, _no_tangents,
-                     _ref, _rows, _table, _vector)
+from ._serve import (_I32, _I64, _P, RotaryPlan, _allocating_on, _Function, _like, _moved,
+                     _no_tangents, _ref, _rows, _table, _vector)
 
 HEADER = os.path.join(os.path.dirname(_lib.PKG), "include", "e2s_step.h")
 
@@ -168,7 +168,8 @@ def _forward(inputs, q, k, positions, plan, q_weight, k_weight, q_out, k_out, st
             st = _rows(o, name + "_out", t.dtype)[:3]
             if o.shape != t.shape:
                 raise ValueError(f"{name}_out must have {name}'s shape")
-            if o.data_ptr() == t.data_ptr() and list(st) != strides[3 * i:3 * i + 3]:
+            if o.data_ptr() == t.data_ptr() and \
+                    _moved(t.shape, tuple(strides[3 * i:3 * i + 3]), st):
                 raise ValueError(f"{name}_out in the place of {name} must have its strides")
             out_strides += st
         outs.append(o)
