@@ -263,3 +263,70 @@ def filled(rng, B, G, P, D, lengths, spare=2, bad=None, spread=2.0):
                 for _ in range(2))
         pool.append(list(table[b]), 0, k, v)
     return pool, table
+
+
+def held_rows(tables, row_of_pages, n):
+    """The first n cached tokens of a sequence by (k, k_scale, v, v_scale) and its row of the
+    page table, all on one device: keys and values [Hkv, n, d] and the values' scales [Hkv, n] in
+    float64, and which tokens have a page [n] (what the others hold is zeros)."""
+    k, ks, v, vs = tables
+    P, D = k.shape[2], 2 * k.shape[3]
+    i = torch.arange(n, device=k.device)
+    page, row = row_of_pages.to(k.device).long()[i // P], i % P
+    there = (page >= 0) & (page < k.shape[0])
+    page = torch.where(there, page, 0)
+    grid = torch.from_numpy(np.concatenate([GRID, -GRID])).to(k.device)
+    byte = k[page, :, row]                                             # [n, Hkv, d / 2]
+    codes = torch.stack([byte & 15, byte >> 4], -1).flatten(-2)
+    e = ks[page, :, row // 16, row % 4, :, row % 16 // 4].double()     # [n, Hkv, d / 32]
+    scale = torch.where(e == 255, math.nan, torch.exp2(e - 127)).repeat_interleave(32, -1)
+    keys = grid[codes.long()] * scale
+    byte = v[page, :, row // 32, :, row % 32 // 2]                     # [n, Hkv, d]
+    codes = torch.where((row % 2 == 1)[:, None, None], byte >> 4, byte & 15)
+    s = vs[page, :, row].double()                                      # [n, Hkv]
+    values = grid[codes.long()] * s[..., None]
+    none = ~there
+    keys[none], values[none], s[none] = 0.0, 0.0, 0.0
+    return keys.transpose(0, 1), values.transpose(0, 1), s.t(), there
+
+
+def attend_rows(held, q, count, kind, causal=True, scale=None):
+    """attend() of one sequence, from held_rows() and its queries q [H, T, d] in float64 on the
+    same device: outputs [H, T, d] (queries behind the count: zeros) and their tolerances."""
+    k, v, s, there = held
+    G, n, D = k.shape
+    H, T = q.shape[:2]
+    scale = D ** -0.5 if scale is None else scale
+    half = R.HALF_STEP[DTYPES[kind]]
+    if n == 0:
+        return torch.zeros_like(q), torch.zeros_like(q)
+    x = q.reshape(G, H // G * T, D)
+    t = torch.arange(T, device=q.device).repeat(H // G)
+    limit = n - (count - 1 - t) if causal else torch.full_like(t, n)
+    limit = torch.where(t < count, limit, 0)
+    seen = there & (torch.arange(n, device=q.device) < limit[:, None])         # [rows, n]
+    some = seen.any(-1)[:, None]
+
+    def times(a, b):                                     # [G, rows, d] by [G, n, d]
+        return torch.matmul(a, b.transpose(1, 2).contiguous())
+
+    def most(a):                                         # of what is seen, zeros of nothing
+        return torch.where(seen, a, 0.0).amax(-1, keepdim=True)
+    logit = torch.where(seen, times(x, k) * scale, -math.inf)
+    p = torch.exp(logit - torch.where(some, logit.amax(-1, keepdim=True), 0.0))
+    p = p / torch.where(some, p.sum(-1, keepdim=True), 1.0)
+    out, mag = torch.matmul(p, v), torch.matmul(p, v.abs())
+    top = x.abs().reshape(G, -1, D // 32, 32).amax(-1).repeat_interleave(32, -1)
+    dots = most(times(x.abs(), k.abs())) * scale
+    miss = most(times(top, k.abs())) * scale * Q_FLOOR[kind]
+    err = 2 * (D * U * dots + miss + 4 * U * most(logit.abs()) * 1.45 + 2.0 ** -22 +
+               (n / 32 + 64) * U)
+    blocks = -(-n // 128)
+    pad = blocks * 128 - n
+    weight = torch.nn.functional.pad(p * s[:, None], (0, pad)).unflatten(-1, (blocks, 128))
+    number = torch.nn.functional.pad(seen.double(), (0, pad)).unflatten(-1, (blocks, 128)).sum(-1)
+    low = (weight.amax(-1) * 6 * number).sum(-1, keepdim=True)
+    tol = (half * torch.clamp(out.abs(), min=R.TINY[DTYPES[kind]]) + mag * (P_STEP[kind] + err) +
+           P_FLOOR[kind] * low)
+    tol = torch.where(some, tol, 0.0)
+    return out.reshape(H, T, D), tol.reshape(H, T, D)
