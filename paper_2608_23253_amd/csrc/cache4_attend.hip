@@ -27,12 +27,18 @@
 // part its keys and merge in LDS; keys are split over workgroups where there are few rows, and
 // attend4_join_kernel joins the parts.
 //
-// What bounds it: a decoding step reads 133 bytes per token and key head (d = 128, of 258 in 8
-// bits), of which 4 sequences of 60000 to 131072 keys take 35 us (4.8 TB/s) and 64 of 130 to
-// 1200 keys, 32 heads, f16, 48 us; with many rows the vector unit, some 410 instructions to a
-// step beside 40 matrix products (1300 cycles): 2 x 1024 queries of 2048 keys, 28 heads, bf16: 79
-// to 89 us, 510 to 570 TFLOP/s of the 45 GFLOP that the mask leaves.  Two waves to a SIMD (213
-// registers) hold a step's keys and values: three waves spilled (107 us for 91).  What the
+// What bounds it.  A decoding step reads 133 bytes per token and key head (d = 128, of 258 in 8
+// bits): 64 sequences of 4096 keys, 32 heads, take 196 us (5.75 TB/s; f16 200, f32 209).  Of 4
+// sequences of 60000 to 131072 keys this kernel takes 35 us (4.8 TB/s) and the join 5, of 64 of 130
+// to 1200 keys, 32 heads, f16, 46: there the longest wave's steps.
+// With many rows neither unit is full: 2 x 1024 queries of 2048 keys, 28 heads, bf16, take 78 to
+// 90 us (f16 97, f32 136), 500 to 580 TFLOP/s of the 45 GFLOP that the mask leaves.  Those are
+// 44800 steps of 504 vector instructions and 40 matrix products.  By counters the vector unit is at
+// work for 54 % of the time and the matrix unit for 28 %; a SIMD has 1.3 waves on average of the
+// two that fit (3584 waves of 9 to 16 steps on 2048 places), and a wave alone seldom has products
+// and conversions under way at once.  Waves wait 35 % of their time for a turn to issue, 16 % for
+// what they read.  Two waves to a SIMD (213 registers) hold a step's keys and values: three
+// waves spilled (107 us for 91).  What the
 // steps of making it fast gave for the 1024 queries, in us: 155 as first written; 116 with two
 // waves to a SIMD; 102 with loops that leave keys and outputs in place; 91 with addresses from
 // one lookup a segment and maxima without the compiler's quieting; 89 with the values' loads
@@ -333,7 +339,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend4_kernel(
         a.k_scale + (n16 >> 2 & 1) * (D / 2) + ((n16 & 3) * (D / 32) + k_block) * 4;
     const uint8_t* const v_lane = a.v + n16 * 16;
     const uint16_t* const vs_lane = a.v_scale + 16 * (g4 & 1);
-    const bool v_far = (g4 & 2) != 0;
     // the lane (times 4) of its keys', its values' and its values' scales' first group in a segment
     const int k_from = (n16 >> 3) * 4, v_from = g4 * 4, vs_from = (g4 >> 1) * 4;
     auto fetch_k = [&](const Segment& w, int key) {      // key: of the segment

@@ -4,24 +4,27 @@
 //   y = turned(x r w),  r = 1 / sqrt(mean(x^2) + eps)
 //   back: g = turned back(grad), u = g w, dx = r (u - x r mean(u x r)), dw = sum g x r
 //
-// Streams: forward reads and writes every element once, back reads two and writes one, so the
-// copy rate bounds both.  As in the rotation alone, a workgroup takes a run of TT tokens of one
-// sequence for all heads: cosines and sines of the run go to LDS once, and a thread keeps
-// those of its pairs in registers while it walks over the heads.  A unit is two chunks of W
-// elements of a row that turn together (see rotary.hip), so the rotation stays in a lane; the
-// units of a row are neighbouring lanes, LPR (a power of two) of them, which add the squares
-// up across the row by DPP: no LDS and no second look at the row.
+// Streams: forward reads and writes every element once, back reads two and writes one, so what
+// bounds both is a copy: of 1 GiB 5.8 TB/s, 6.3 with non-temporal loads and stores.  As in the
+// rotation alone, a workgroup takes a run of TT tokens of one sequence for all heads: cosines and
+// sines of the run go to LDS once, and a thread keeps those of its pairs in registers while it
+// walks over the heads.  A unit is two chunks of W elements of a row that turn together (see
+// rotary.hip), so the rotation stays in a lane; the units of a row are neighbouring lanes, LPR (a
+// power of two) of them, which add the squares up across the row by DPP: no LDS and no second look
+// at the row.
 //
 // Each thread's next rows are under way while it turns the present ones, its first ones while
 // cosines and sines are made: 1.07 GB forward (32768 tokens of 64 heads, bf16) take 198 us, 5.4
-// TB/s (a copy of as much 5.1), 249 us without; 336 MB 67 us; back, 503 MB take 114 us, 4.4 TB/s,
-// 145 without.  Back keeps to 168 registers, three waves to a SIMD (174 as the compiler
-// chose, two waves: 125 us; 128 with spills: 196).
+// TB/s, 249 us without; 336 MB 67 us; back, 503 MB take 105 to 114 us, 4.4 to 4.8 TB/s, 145
+// without.  Float32 of few heads is further off: 76 MB (5331 tokens of 14 heads) take 20.5 us, 3.7
+// TB/s, where a thread has one or two rows behind a table of angles in 64 bits.  Back keeps to 168
+// registers, three waves to a SIMD (174 as the compiler chose, two waves: 125 us; 128 with spills:
+// 196).
 //
 // The weights' gradients: a thread owns its unit's columns of every row it walks over, a
 // workgroup joins its threads' in LDS and stores one partial row per tensor, and a second
 // launch adds the partial rows up in order.  Back, a workgroup takes several runs, so that
-// at most kMostParts partial rows exist.
+// at most kNormMostParts partial rows exist.
 #include "serve_device.h"
 #include "step_kernels.h"
 

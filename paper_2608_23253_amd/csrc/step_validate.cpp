@@ -147,15 +147,25 @@ Attend4Plan attend4_plan(const e2s_cache4& c, const e2s_cache4_attend_shape& s) 
     p.rows = static_cast<int64_t>(s.num_heads) / G * s.num_queries;
     p.row_groups = (p.rows + 15) / 16;
     const int64_t units = B * G * p.row_groups;
-    // The device holds 2048 waves at two to a SIMD.  From as many units on, each is one wave, and
-    // nothing is joined (64 sequences of up to 1200 keys, 32 heads: 47 us; two waves 47, four 53).
-    // Fewer units part their keys, in workgroups of two or four waves, until four or three waves
-    // for each SIMD are there, more than fit, as lengths are mostly shorter than the longest: 1344
-    // units (16 sequences of up to 4200 keys, ragged counts) take 38 us with four, 45 with three,
-    // 52 with four waves to a workgroup; 16 units of up to 131072 keys 35 us with three, 37 with
-    // two, 44 with four, and 43 in workgroups of two.  Short sequences of few units: one workgroup
-    // of eight waves has all keys (one of up to 1100 keys, 4 key heads: 8.0 us; in parts 6.0 and a
-    // join of 3.3).
+    // The device holds 2048 waves at two to a SIMD.  Times of one query of 7 heads to each of 4
+    // key heads, d = 128, bf16, by units and longest length; "even": all sequences as long,
+    // "ragged": any length up to it.
+    //   Eight waves, which have all keys of a unit, for few short sequences: at 16 x 1100 9.1 us
+    // against 9.9 in parts and joined, at 128 x 1100 9.4 and 11.7, at 252 x 2048 16.6 and 18.7; at
+    // 64 x 2048 11.3 and 10.1.  Beyond 2048 keys they lose (64 x 4096: 17.1 and 14.3) until the
+    // units fill the device (252 x 4096: 25.5 and 30.6); at 256 x 1100 and x 2048 eight would
+    // still be ahead (10.8 for 17.2, 16.7 for 19.2).
+    //   One wave from 2048 units on: 2048 x 1100 even 51 us, of two waves 55, of four 59; ragged
+    // 36, 35, 40; x 4096 even 198, 206, 199; ragged 139, 123, 115.
+    //   Between, parts: workgroups of four or two waves, until there are three or four waves to a
+    // SIMD, more than fit.  16 units of up to 131072 ragged keys take 35 us with three of four
+    // (two 37, four 44, workgroups of two 43), 1344 units (16 sequences of up to 4200 keys and 48
+    // queries, ragged counts) 38 with four of two (three 45, workgroups of four 52).  Neither
+    // number holds everywhere, as whole steps of 128 keys round a wave's share: at 384 x 4096 even
+    // three of four are best (38.6; two 43.7, four 41.6), at 508 x 4096 two of four are (44; three
+    // 56), at 1024 x 2048 even two of two (45; four 54) and at 1536 x 4096 two of four (150; four
+    // of two 188); at 1024 x 512 ragged four of two take 23, two 12.5, one wave 12.9.  A cut by the
+    // lengths that a call has would need neither.
     if (units < 256 && s.max_tokens <= 2048) p.waves = 8;
     else p.waves = units < 512 ? 4 : units < 2048 ? 2 : 1;
     const int64_t unit = static_cast<int64_t>(kStep4) * p.waves;
